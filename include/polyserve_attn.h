@@ -135,9 +135,102 @@ ps_status ps_kv_gather(const ps_kv *kv, const int32_t *block_table_row_dev, int3
 ps_status ps_kv_gather_fp8(const ps_kv *kv, const int32_t *block_table_row_dev, int32_t len, void *k_codes_out_dev,
                            void *v_codes_out_dev, float *k_scale_out_dev, float *v_scale_out_dev, void *stream);
 
-/* Synchronises `stream`, then returns PS_OK or PS_ERR_BOUNDS for the pool's
- * write/gather kernels since the last call, and clears the flag. */
+/* Synchronises `stream`, then returns PS_OK, PS_ERR_BOUNDS or PS_ERR_TIMEOUT for
+ * the kernels of the pool that have no plan (write, gather, the calls of a
+ * speculative step) since the last call, and clears the flag. */
 ps_status ps_kv_status(ps_kv *kv, void *stream);
+
+/* ------------------------------------------------------------------------ */
+/* A speculative step over the paged cache.  (The paper batches one new token */
+/* per decode request; its section 2.1 cache and section 2.4 batch are what    */
+/* these calls work on.)                                                       */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * Append with the norms of queries and keys for each head and the position
+ * rotation in the same pass.  For token t of the batch and each of its heads
+ *     y = x / sqrt(mean(x^2) + eps) * weight           (q, k; where a weight is given)
+ *     (a, b) -> (a cos - b sin, b cos + a sin)          (q, k; the first rot_dim elements)
+ * with row position(t) of cos_sin_dev holding rot_dim / 2 cosines and then
+ * rot_dim / 2 sines.  A pair is (x[i], x[i + rot_dim / 2]), or with interleaved
+ * != 0 (x[2 i], x[2 i + 1]).  q goes to q_out_dev, k and (as it is) v to their
+ * pages as ps_kv_write puts them, in an FP8 pool quantised from the rotated
+ * fp32 key.  Arithmetic is fp32; every result is rounded once.
+ */
+typedef struct {
+    const void *q_dev;          /* bf16, token t at q_dev + t * q_stride: [n_q_heads, head_dim] */
+    const void *k_new_dev;      /* bf16 [n_kv_heads, head_dim] a token */
+    const void *v_new_dev;      /* bf16 [n_kv_heads, head_dim] a token */
+    void *q_out_dev;            /* bf16 [T, n_q_heads, head_dim]; may be q_dev itself where that is packed */
+    int64_t q_stride;           /* elements from one token to the next, a multiple of 8; 0 = packed */
+    int64_t k_stride;
+    int64_t v_stride;
+    const void *q_weight_dev;   /* bf16 [head_dim], or NULL: no norm */
+    const void *k_weight_dev;
+    const float *cos_sin_dev;   /* fp32 [n_positions, rot_dim] */
+    const int32_t *positions_dev; /* int32 [T], or NULL: position(t) is the token's position in its sequence */
+    int64_t n_positions;
+    int32_t rot_dim;            /* a multiple of 16, at most head_dim; 0 = no rotation */
+    int32_t interleaved;
+    float eps;
+} ps_rope;
+
+/*
+ * Lengths, block table and stream as for ps_kv_write.  All tensors 16-byte
+ * aligned.  Asynchronous on `stream`.  Errors: PS_ERR_INVALID, PS_ERR_UNSUPPORTED
+ * (rot_dim), PS_ERR_CUDA; a token whose page lies outside the pool or whose
+ * position lies outside the table is skipped, q_out's row included, and
+ * reported by ps_kv_status.
+ */
+ps_status ps_kv_write_rope(ps_kv *kv, const ps_rope *args, const int32_t *block_table_dev, int32_t max_pages, const int32_t *prior_host,
+                           const int32_t *q_len_host, int32_t n, void *stream);
+
+/*
+ * Attention for trees of drafted tokens.  Request r has prior[r] >= 0 tokens
+ * of context and n_nodes[r] in 1 .. 64 * mask_words drafted ones, node i cached
+ * at position prior[r] + i.  Node i sees the whole context and node j where bit
+ * j % 64 of word j / 64 of its mask row is set, its own bit like any other
+ * (mask_dev: [T, mask_words], mask_words in 1 .. 4; bits from n_nodes[r] on are
+ * not looked at).  q, out and lse as for ps_attn_run, with T = sum n_nodes.  A
+ * node that sees nothing gets zeros and lse = -inf.  What a node does not see
+ * has no part in its result, whatever values it holds.
+ *
+ * bf16 pools.  workspace_dev: 256-byte aligned device memory of
+ * ps_attn_tree_workspace bytes, which depend on the shape alone; scratch, no
+ * initialisation.  Calls that use one workspace are issued to one stream or
+ * ordered by the caller.  Asynchronous on `stream`; may be captured into a
+ * CUDA graph, which replays these lengths and pointers.  Errors: PS_ERR_INVALID,
+ * PS_ERR_UNSUPPORTED, PS_ERR_WORKSPACE, PS_ERR_CUDA; pages outside the pool read
+ * as zeros, and they and waits that ran out are reported by ps_kv_status.
+ */
+ps_status ps_attn_tree_workspace(const ps_shape *shape, size_t *bytes_out);
+ps_status ps_attn_tree(const ps_kv *kv, const void *q_dev, const int32_t *block_table_dev, int32_t max_pages, const int64_t *mask_dev,
+                       int32_t mask_words, const int32_t *prior_host, const int32_t *n_nodes_host, int32_t n, void *out_dev,
+                       float *lse_out_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* Bound of every wait inside ps_attn_tree's kernels, as ps_plan_set_wait_limit's. */
+ps_status ps_kv_set_wait_limit(ps_kv *kv, int64_t limit_ns);
+
+/*
+ * Keep an accepted path: position prior[r] + i receives the K and V of position
+ * prior[r] + index[r][i], for i < count[r].  index_dev: int32 [n, index_stride],
+ * strictly increasing over a row's first count entries and below n_nodes[r];
+ * count_dev: int32 [n], 0 .. min(n_nodes[r], index_stride).  Positions behind
+ * the path keep what they hold.  A request whose path is none is left as it is,
+ * as is a token whose page lies outside the pool, and reported by
+ * ps_kv_status.  Stored tokens are copied bit for bit.  Asynchronous.
+ */
+ps_status ps_kv_accept(ps_kv *kv, const int32_t *block_table_dev, int32_t max_pages, const int32_t *prior_host, const int32_t *n_nodes_host,
+                       int32_t n, const int32_t *index_dev, int32_t index_stride, const int32_t *count_dev, void *stream);
+
+/*
+ * Read tokens begin[r] .. begin[r] + len[r] (len >= 0) of n sequences back, packed as
+ * bf16 [sum len, n_kv_heads, head_dim] (either output may be NULL): a bf16 pool's
+ * bit for bit, an FP8 pool's as code * scale rounded to bf16.  Tokens whose page
+ * lies outside the pool are left unwritten and reported by ps_kv_status.
+ */
+ps_status ps_kv_read(const ps_kv *kv, const int32_t *block_table_dev, int32_t max_pages, const int32_t *begin_host, const int32_t *len_host,
+                     int32_t n, void *k_out_dev, void *v_out_dev, void *stream);
 
 /* ------------------------------------------------------------------------ */
 /* Work partition (host only).                                                */

@@ -35,6 +35,14 @@ class ps_shape(ctypes.Structure):
                 ("page_size", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
+class ps_rope(ctypes.Structure):
+    _fields_ = [("q_dev", ctypes.c_void_p), ("k_new_dev", ctypes.c_void_p), ("v_new_dev", ctypes.c_void_p), ("q_out_dev", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("q_weight_dev", ctypes.c_void_p), ("k_weight_dev", ctypes.c_void_p), ("cos_sin_dev", ctypes.c_void_p),
+                ("positions_dev", ctypes.c_void_p), ("n_positions", ctypes.c_int64), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
 class ps_plan_opts(ctypes.Structure):
     _fields_ = [("decode_segment_tokens", ctypes.c_int32), ("prefill_segment_tokens", ctypes.c_int32),
                 ("num_sms", ctypes.c_int32)]
@@ -68,6 +76,7 @@ class ps_grid_row(ctypes.Structure):
 EXPORTS = ["ps_kv_bytes", "ps_kv_alloc", "ps_kv_free", "ps_kv_write", "ps_kv_gather", "ps_kv_gather_fp8", "ps_kv_status", "ps_attn_plan",
            "ps_plan_free", "ps_plan_get_info", "ps_plan_get_items", "ps_attn_run", "ps_plan_status",
            "ps_plan_set_timing", "ps_plan_get_timing", "ps_plan_set_wait_limit", "ps_profile_grid", "ps_attn_run_static",
+           "ps_kv_write_rope", "ps_attn_tree_workspace", "ps_attn_tree", "ps_kv_set_wait_limit", "ps_kv_accept", "ps_kv_read",
            "ps_last_error", "ps_version"]
 
 _lib = None
@@ -93,6 +102,12 @@ def load() -> ctypes.CDLL:
     lib.ps_kv_gather.argtypes = [_vp, _vp, _i32, _vp, _vp, _vp]
     lib.ps_kv_gather_fp8.argtypes = [_vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp]
     lib.ps_kv_status.argtypes = [_vp, _vp]
+    lib.ps_kv_write_rope.argtypes = [_vp, ctypes.POINTER(ps_rope), _vp, _i32, _vp, _vp, _i32, _vp]
+    lib.ps_attn_tree_workspace.argtypes = [sp, ctypes.POINTER(_sz)]
+    lib.ps_attn_tree.argtypes = [_vp, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _sz, _vp]
+    lib.ps_kv_set_wait_limit.argtypes = [_vp, _i64]
+    lib.ps_kv_accept.argtypes = [_vp, _vp, _i32, _vp, _vp, _i32, _vp, _i32, _vp, _vp]
+    lib.ps_kv_read.argtypes = [_vp, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp]
     lib.ps_attn_plan.argtypes = [sp, _vp, _vp, _i32, _i32, ctypes.POINTER(ps_plan_opts), ctypes.POINTER(_vp),
                                  ctypes.POINTER(_sz)]
     lib.ps_plan_free.argtypes = [_vp]
@@ -203,6 +218,47 @@ def ps_kv_gather(kv, block_table_row_dev, length, k_out_dev, v_out_dev, stream=N
 def ps_kv_gather_fp8(kv, block_table_row_dev, length, k_codes_out_dev, v_codes_out_dev, k_scale_out_dev, v_scale_out_dev, stream=None):
     _check(load().ps_kv_gather_fp8(kv, _ptr(block_table_row_dev), length, _ptr(k_codes_out_dev), _ptr(v_codes_out_dev),
                                    _ptr(k_scale_out_dev), _ptr(v_scale_out_dev), _ptr(stream)))
+
+
+def _batch(prior_host, len_host):
+    """The two length arrays of a batch and its number of requests."""
+    a, b = lengths(prior_host), lengths(len_host)
+    if a.ndim != 1 or b.ndim != 1 or a.shape != b.shape:
+        raise ValueError("one length a request in both arrays: got %s and %s" % (a.shape, b.shape))
+    return a, b, a.shape[0]
+
+
+def ps_kv_write_rope(kv, args: ps_rope, block_table_dev, max_pages, prior_host, q_len_host, stream=None):
+    a, b, n = _batch(prior_host, q_len_host)
+    _check(load().ps_kv_write_rope(kv, ctypes.byref(args), _ptr(block_table_dev), max_pages, a.ctypes.data, b.ctypes.data, n, _ptr(stream)))
+
+
+def ps_attn_tree_workspace(shape: ps_shape) -> int:
+    out = _sz(0)
+    _check(load().ps_attn_tree_workspace(ctypes.byref(shape), ctypes.byref(out)))
+    return out.value
+
+
+def ps_attn_tree(kv, q_dev, block_table_dev, max_pages, mask_dev, mask_words, prior_host, n_nodes_host, out_dev, lse_out_dev, workspace_dev,
+                 workspace_bytes, stream=None):
+    a, b, n = _batch(prior_host, n_nodes_host)
+    _check(load().ps_attn_tree(kv, _ptr(q_dev), _ptr(block_table_dev), max_pages, _ptr(mask_dev), mask_words, a.ctypes.data, b.ctypes.data, n,
+                               _ptr(out_dev), _ptr(lse_out_dev), _ptr(workspace_dev), workspace_bytes, _ptr(stream)))
+
+
+def ps_kv_set_wait_limit(kv, limit_ns: int):
+    _check(load().ps_kv_set_wait_limit(kv, limit_ns))
+
+
+def ps_kv_accept(kv, block_table_dev, max_pages, prior_host, n_nodes_host, index_dev, index_stride, count_dev, stream=None):
+    a, b, n = _batch(prior_host, n_nodes_host)
+    _check(load().ps_kv_accept(kv, _ptr(block_table_dev), max_pages, a.ctypes.data, b.ctypes.data, n, _ptr(index_dev), index_stride, _ptr(count_dev),
+                               _ptr(stream)))
+
+
+def ps_kv_read(kv, block_table_dev, max_pages, begin_host, len_host, k_out_dev, v_out_dev, stream=None):
+    a, b, n = _batch(begin_host, len_host)
+    _check(load().ps_kv_read(kv, _ptr(block_table_dev), max_pages, a.ctypes.data, b.ctypes.data, n, _ptr(k_out_dev), _ptr(v_out_dev), _ptr(stream)))
 
 
 def ps_kv_status(kv, stream=None):

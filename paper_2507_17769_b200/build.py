@@ -54,7 +54,8 @@ def build_torch_calls(force: bool = False, build: bool = True) -> str:
     import torch
 
     path, src = torch_calls_path(), os.path.join(CSRC, "torch_calls.cpp")
-    if not build or (not force and os.path.exists(path) and os.path.getmtime(path) >= os.path.getmtime(src)):
+    sources = [src, os.path.join(HERE, "..", "include", "polyserve_attn.h")]
+    if not build or (not force and os.path.exists(path) and os.path.getmtime(path) >= max(map(os.path.getmtime, sources))):
         return path
     root = os.path.dirname(torch.__file__)
     tmp = path + ".tmp.%d" % os.getpid()

@@ -6,7 +6,7 @@
 #include <new>
 #include <vector>
 
-#include "common.cuh"
+#include "kv_rows.cuh"
 
 namespace ps {
 
@@ -37,36 +37,6 @@ ps_status check_shape(const ps_shape* s) {
     return PS_OK;
 }
 
-// Where the new tokens go: request r's are packed tokens q_start[r] .. q_start[r + 1] and follow prior[r] cached ones.  The
-// lengths travel as a kernel parameter: copied to the device first they cost every append a small transfer that its stream
-// has to wait for (about 6 us between two kernels, and 4 us of host time).  Batches of more than kParamRowsMax requests
-// still take that way.
-template <int N>
-struct ParamRows {
-    int32_t q_start_[N + 1], prior_[N];
-    __device__ __forceinline__ int q_start(int r) const { return q_start_[r]; }
-    __device__ __forceinline__ int prior(int r) const { return prior_[r]; }
-};
-struct DeviceRows {
-    const int32_t *q_start_, *prior_;
-    __device__ __forceinline__ int q_start(int r) const { return q_start_[r]; }
-    __device__ __forceinline__ int prior(int r) const { return prior_[r]; }
-};
-constexpr int kParamRowsMax = 4000;  // 32 KB, as much as a kernel's parameters may be
-
-// request of packed token t: last r with q_start(r) <= t
-template <class Rows>
-__device__ __forceinline__ int request_of(const Rows& rows, int n, int t) {
-    // (up to the first request of several tokens, which in a serving batch come last, every request has one)
-    if (t < n && rows.q_start(t) == t) return t;
-    int lo = 0, hi = n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (rows.q_start(mid) <= t) lo = mid; else hi = mid - 1;
-    }
-    return lo;
-}
-
 // Append and gather are copies between a token's row [Hkv][d] and its place in a page, so they are bound by memory, and at
 // these sizes by its latency: a warp moves one token's K and V, 32 bytes a lane, with all loads of a chunk (two pairs of K
 // and of V a lane) under way before its first store.  A 16-byte unit u of token slot t lies at u ^ (t & 7): a pair of units
@@ -75,44 +45,6 @@ __device__ __forceinline__ int request_of(const Rows& rows, int n, int t) {
 // 16-byte unit and a request search in each, 20.6 with two tokens a warp, 19.3 with one, 15.2 (4.9 TB/s) launched early.
 constexpr int kCopyThreads = 256;
 constexpr int kCopyTokens = kCopyThreads / 32;  // of a CTA
-
-struct Pair32 {
-    uint4 a, b;
-};
-__device__ __forceinline__ Pair32 load32(const void* p) {
-    Pair32 x;
-    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(x.a.x), "=r"(x.a.y), "=r"(x.a.z), "=r"(x.a.w), "=r"(x.b.x), "=r"(x.b.y), "=r"(x.b.z), "=r"(x.b.w)
-                 : "l"(p));
-    return x;
-}
-__device__ __forceinline__ void store32(void* p, const Pair32& x) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(x.a.x), "r"(x.a.y), "r"(x.a.z), "r"(x.a.w),
-                 "r"(x.b.x), "r"(x.b.y), "r"(x.b.z), "r"(x.b.w)
-                 : "memory");
-}
-// a token's row: 32-byte aligned where the caller's tensor is (ALIGNED), else 16
-template <bool ALIGNED>
-__device__ __forceinline__ Pair32 load_row32(const char* p) {
-    if (ALIGNED) return load32(p);
-    return Pair32{reinterpret_cast<const uint4*>(p)[0], reinterpret_cast<const uint4*>(p)[1]};
-}
-template <bool ALIGNED>
-__device__ __forceinline__ void store_row32(char* p, const Pair32& x) {
-    if (ALIGNED) {
-        store32(p, x);
-    } else {
-        reinterpret_cast<uint4*>(p)[0] = x.a;
-        reinterpret_cast<uint4*>(p)[1] = x.b;
-    }
-}
-__device__ __forceinline__ Pair32 swap_if(const Pair32& x, bool odd) { return odd ? Pair32{x.b, x.a} : x; }
-// 32-byte pair c of a token's row -> offset of its (page, kv head)'s pair in the K block, from the page's start
-template <int D>
-__device__ __forceinline__ uint32_t pair_offset(int c, int slot) {
-    constexpr int kPairs = D / 16;
-    return (uint32_t)(c / kPairs) * (uint32_t)page_head_bytes(D) + (unit_offset(slot, (c % kPairs) * 16) & ~16u);
-}
 
 template <int D, bool ALIGNED, class Rows>
 __global__ void __launch_bounds__(kCopyThreads) kv_write_kernel(char* pool, int64_t num_pages, const char* __restrict__ k_new, const char* __restrict__ v_new,
@@ -200,13 +132,6 @@ __global__ void __launch_bounds__(kCopyThreads) kv_gather_kernel(const char* poo
 // when later tokens are appended.  (With 8 significant bits a softmax weight of exactly 1 times the scale is still
 // exact in the 16-bit operand of the decode kernel's MMA.)
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t quantise4(float x0, float x1, float x2, float x3, float scale) {
-    uint16_t lo, hi;  // cvt packs its first operand into the upper byte
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(__fdiv_rn(x1, scale)), "f"(__fdiv_rn(x0, scale)));
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(__fdiv_rn(x3, scale)), "f"(__fdiv_rn(x2, scale)));
-    return (uint32_t)lo | ((uint32_t)hi << 16);
-}
-
 // One warp quantises K and V of one (new token, kv head): lane l holds elements 4 l .. 4 l + 3 (head_dim = 128).
 template <class Rows>
 __global__ void kv_write_fp8_kernel(char* pool, int64_t num_pages, const uint2* __restrict__ k_new,
@@ -237,10 +162,7 @@ __global__ void kv_write_fp8_kernel(char* pool, int64_t num_pages, const uint2* 
             float amax = fmaxf(fmaxf(fabsf(x0), fabsf(x1)), fmaxf(fabsf(x2), fabsf(x3)));
 #pragma unroll
             for (int o = 16; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-            float scale = amax > 0.f ? __fdiv_rn(amax, 448.f) : 1.f;
-            uint32_t sbits = __float_as_uint(scale);  // rounded up to 8 significant bits
-            if (sbits & 0xffffu) sbits = (sbits | 0xffffu) + 1u;
-            scale = __uint_as_float(sbits);
+            const float scale = fp8_scale(amax);
             *reinterpret_cast<uint32_t*>(blk + kv * (kPage * d) + off) = quantise4(x0, x1, x2, x3, scale);
             if (lane == 0) reinterpret_cast<float*>(blk + 2 * kPage * d)[kv * kPage + slot] = scale;
         }
@@ -362,6 +284,7 @@ ps_status ps_kv_alloc(const ps_shape* shape, int64_t num_pages, void* dev_mem, s
     kv->p.base = (char*)dev_mem;
     kv->p.meta_dev = nullptr;
     kv->p.flag_dev = nullptr;
+    kv->p.wait_limit_ns = kDefaultWaitLimitNs;
     kv->p.meta_cap = 1 << 16;
     if (kv->p.owned) {
         cudaError_t e = cudaMalloc((void**)&kv->p.base, need);
@@ -458,7 +381,8 @@ ps_status ps_kv_status(ps_kv* kv, void* stream) {
     PS_CUDA_TRY(cudaMemcpy(&flag, kv->p.flag_dev, sizeof flag, cudaMemcpyDeviceToHost));
     if (flag) {
         PS_CUDA_TRY(cudaMemset(kv->p.flag_dev, 0, sizeof flag));
-        return fail(PS_ERR_BOUNDS, "a block-table entry pointed outside the pool; that token was skipped");
+        if (flag & kStatusTimeout) return fail(PS_ERR_TIMEOUT, "a bounded wait inside the tree attention kernel expired; its output is invalid");
+        return fail(PS_ERR_BOUNDS, "a block-table entry pointed outside the pool, a position outside the table of angles, or an accepted path outside its tree; what it concerned was skipped");
     }
     return PS_OK;
 }

@@ -1,0 +1,926 @@
+// Attention for a tree of drafted tokens over the paged cache.
+//
+// Token i of request r (its node i, cached at position prior + i) attends the request's whole context, keys 0 .. prior - 1, and the
+// tree tokens that its mask row names, bit j for node j:
+//     out[i, h] = sum_k softmax_k(q[i, h] . K[k, g] / sqrt(d)) V[k, g],   lse[i, h] = log sum_k exp(q . K[k, g] / sqrt(d)).
+// All nodes of a tree read the same context, so with few nodes the kernel is bound by the bytes of K and V (4 d nodes G
+// operations for 4 d bytes of a token and kv head: 148 SMs' tensor cores and HBM meet at some 250 (node, head) rows).  It streams
+// every K and V tile once and runs both products on the 5th-generation tensor cores, whose 128 rows are the (node, head) pairs that
+// share a kv head.
+//
+// Work: an item is one (request, kv head, group of up to 256 rows).  Its keys are tiles of 128, and all items' tiles, with
+// kItemUnits more an item for its start and end, make one line that is cut into equal shares, a CTA each, wherever the cuts fall
+// (stream-K).  So one request on a long context, or a ragged batch, fills all SMs, and a CTA has at most two pieces of an item:
+// partial rows go to fixed places of the workspace and tree_merge_kernel joins them in the order of their keys.  The shares
+// follow from the batch's lengths, which travel as kernel parameters: there is no work list to upload and nothing to
+// initialise.
+//
+//   warps 0-3, 4-7  softmax of streams 0 and 1.  The steps (key tile x q tile of 128 rows) of all items alternate between the
+//                   two, so that one stream's exponentials run under the other's products.  With two q tiles each stream keeps one;
+//                   with one q tile the streams take key tiles in turn, with a running maximum, sum and accumulator each, joined
+//                   when the item ends.  Thread t owns row t (TMEM lane t).
+//   warp 8          K and V tiles: pool blocks gathered by tensor map into one ring, in the order of use K0 K1 V0 K2 V1 ...
+//   warp 9          MMA issue: S = Q K^T (operands in shared memory), O += P V (P as bf16 in the columns that S had)
+//   warp 10         Q tiles
+//   warp 11         V tiles that hold tree tokens or the sequence's end: rows behind the end become zero, and rows with
+//                   infinities or NaN too, because 0 * inf would reach nodes that do not see them; their weights are added by
+//                   the rows that do when the item ends.
+//
+// Every wait is bounded; on expiry the CTA flags the pool and drains.
+#include <cuda_fp16.h>
+
+#include "tcgen05.cuh"
+
+namespace ps {
+
+namespace {
+
+constexpr int kThreads = 384;
+constexpr int kRegsSoftmax = 192, kRegsOther = 120;  // 384 x 168 at launch = 256 x 192 + 128 x 120
+constexpr int kLoadWarp = 8, kMmaWarp = 9, kQWarp = 10;  // (11: rows of V)
+constexpr int kTileKeys = 128, kRows = 128;
+constexpr int kGroupRows = 2 * kRows;      // rows of an item
+constexpr int kMaxNodes = 256;
+constexpr int kItemUnits = 1;              // what an item's start and end cost, in key tiles
+constexpr float kRescaleThreshold = 8.f;   // log2 units
+
+template <int D>
+struct Cfg {
+    static constexpr int kHalves = D / 64;
+    static constexpr int kHalfBytes = kTileKeys * 128;
+    static constexpr int kTileBytes = kHalves * kHalfBytes;  // a Q, K or V tile
+    static constexpr int kSlots = D == 128 ? 5 : 10;         // K and V tiles in flight
+    // Items whose flagged tree tokens are kept.  One stream may be one item ahead of the other, PV then stops, and the ring holds V tiles
+    // of kSlots / 2 + 1 items more, of a tile each.
+    static constexpr int kFlagRing = kSlots / 2 + 4;
+    static constexpr int kOffQ = 0;                          // two tiles
+    static constexpr int kOffKV = 2 * kTileBytes;
+    static constexpr int kOffBar = kOffKV + kSlots * kTileBytes;
+    // barrier block
+    static constexpr int kRaw = kSlots / 2 + 2;              // V tiles on their way through warp 11: more than the ring holds
+    static constexpr int full = 0, empty = full + 8 * kSlots, raw = empty + 8 * kSlots, s_full = raw + 8 * kRaw, p_ready = s_full + 16, o_done = p_ready + 16,
+                         q_full = o_done + 16, q_empty = q_full + 16, ex_full = q_empty + 16, ex_free = ex_full + 8, mma_drained = ex_free + 8,
+                         n_bars = (mma_drained + 8) / 8;
+    static constexpr int tmem_slot = 8 * n_bars, abort_slot = tmem_slot + 4, limit_slot = abort_slot + 4, armed = limit_slot + 4;  // slots, Q tiles, V tiles for warp 11
+    static constexpr int flagged = armed + 4 * (kSlots + 2 + kRaw);           // [item % kFlagRing][8]: tree tokens whose V row was taken out
+    static constexpr int exchange = (flagged + kFlagRing * 32 + 7) / 8 * 8;   // [stream][row] (maximum, sum of the weights)
+    static constexpr int rounding = exchange + 2 * kRows * 8;                 // [stream][row] what their rounding adds to the sum, relative, as f16
+    static constexpr int bar_bytes = rounding + 2 * kRows * 2;
+    static constexpr int kSmemBytes = kOffBar + bar_bytes;
+    static_assert(kSmemBytes <= 232448, "shared memory");
+};
+
+// the lengths of a batch
+template <int N>
+struct TreeRows {
+    int32_t q_start[N + 1], unit_start[N + 1], prior[N];
+};
+constexpr int kTreeRowsMax = 2600;  // 31 KB of kernel parameters
+
+struct TreeParams {
+    const __nv_bfloat16* q;
+    const int32_t* block_table;
+    const uint32_t* mask;   // 2 * mask_words 32-bit words a token
+    const char* pool;
+    __nv_bfloat16* out;
+    float* lse;
+    float4* part_ml;        // [2 CTAs][256 rows]
+    float* part_o;
+    int* flag;
+    int64_t num_pages;
+    uint32_t wait_limit_ns;
+    int32_t max_pages, mask_words, n, Hq, Hkv, G, units;
+};
+
+// pieces of items in a CTA's share of the line
+struct Piece {
+    int r, head, q_tok, n_tok, tok0, nodes, prior, kv_len;
+    int tile0, tile1, tiles;
+    __device__ __forceinline__ int n_x(int G) const { return n_tok * G > kRows ? 2 : 1; }
+    __device__ __forceinline__ bool whole() const { return tile0 == 0 && tile1 == tiles; }
+    // first tile with tree tokens or the sequence's end in it
+    __device__ __forceinline__ int tree_tile() const { return prior / kTileKeys; }
+};
+__device__ __forceinline__ int share_begin(int units, int c, int n_cta) { return (int)((int64_t)units * c / n_cta); }
+
+template <class Rows>
+struct PieceIter {
+    const Rows& rows;
+    int n, G, u, end, r;
+    __device__ __forceinline__ PieceIter(const Rows& rows_, int n_, int G_, int u_, int end_) : rows(rows_), n(n_), G(G_), u(u_), end(end_) {
+        int lo = 0, hi = n - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (rows.unit_start[mid] <= u) lo = mid; else hi = mid - 1;
+        }
+        r = lo;
+    }
+    __device__ __forceinline__ bool next(Piece& x) {
+        while (u < end) {
+            while (u >= rows.unit_start[r + 1]) ++r;
+            x.r = r;
+            x.prior = rows.prior[r];
+            x.q_tok = rows.q_start[r];
+            x.nodes = rows.q_start[r + 1] - x.q_tok;
+            x.kv_len = x.prior + x.nodes;
+            x.tiles = (x.kv_len + kTileKeys - 1) / kTileKeys;
+            const int per = x.tiles + kItemUnits, o = u - rows.unit_start[r], item = o / per, w0 = o - item * per, w1 = min(per, w0 + end - u);
+            u += w1 - w0;
+            x.tile0 = max(0, w0 - kItemUnits);
+            x.tile1 = max(0, w1 - kItemUnits);
+            if (x.tile1 <= x.tile0) continue;
+            const int group_tok = kGroupRows / G, groups = (x.nodes + group_tok - 1) / group_tok;
+            x.head = item / groups;
+            x.tok0 = (item - x.head * groups) * group_tok;
+            x.n_tok = min(group_tok, x.nodes - x.tok0);
+            x.q_tok += x.tok0;
+            return true;
+        }
+        return false;
+    }
+};
+
+// 32 bits of a row's mask from node `at` on; nodes before the tree are context and visible, behind its end there is nothing
+__device__ __forceinline__ uint32_t mask_word(const uint32_t* row, int w, int nodes) {
+    const int left = nodes - 32 * w;
+    if (left <= 0) return 0u;
+    const uint32_t x = __ldg(row + w);
+    return left < 32 ? x & ((1u << left) - 1u) : x;
+}
+__device__ __forceinline__ uint32_t mask_bits(const uint32_t* row, int at, int nodes) {
+    if (at <= -32) return 0xffffffffu;
+    if (at < 0) return ((1u << -at) - 1u) | mask_word(row, 0, nodes) << -at;
+    const int w = at >> 5, s = at & 31;
+    const uint32_t lo = mask_word(row, w, nodes);
+    return s == 0 ? lo : __funnelshift_r(lo, mask_word(row, w + 1, nodes), s);
+}
+
+__device__ __forceinline__ bool any_not_finite(const uint4& x) {
+    auto bad = [](uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; };
+    return bad(x.x) || bad(x.y) || bad(x.z) || bad(x.w);
+}
+
+template <int D, class Rows>
+__global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant__ TreeParams p, const __grid_constant__ CUtensorMap q_map,
+                                                            const __grid_constant__ CUtensorMap pool_map, const __grid_constant__ Rows rows) {
+    using C = Cfg<D>;
+    extern __shared__ __align__(1024) char smem[];  // (the 128-byte swizzle wants tiles on 1024 bytes)
+    const uint32_t sbase = smem_u32(smem), bars = sbase + C::kOffBar;
+    volatile int* const s_abort = reinterpret_cast<volatile int*>(smem + C::kOffBar + C::abort_slot);
+    volatile int* const s_armed = reinterpret_cast<volatile int*>(smem + C::kOffBar + C::armed);  // (-1: never; read only after an abort)
+    volatile uint32_t* const s_flagged = reinterpret_cast<volatile uint32_t*>(smem + C::kOffBar + C::flagged);
+    float2* const exchange = reinterpret_cast<float2*>(smem + C::kOffBar + C::exchange);
+    __half* const rounding = reinterpret_cast<__half*>(smem + C::kOffBar + C::rounding);
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::kSlots; ++s) {
+            mbar_init(bars + C::full + 8 * s, 1);
+            mbar_init(bars + C::empty + 8 * s, 1);
+        }
+        for (int s = 0; s < C::kRaw; ++s) mbar_init(bars + C::raw + 8 * s, 1);
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(bars + C::s_full + 8 * x, 1);
+            mbar_init(bars + C::p_ready + 8 * x, 4);
+            mbar_init(bars + C::o_done + 8 * x, 1);
+            mbar_init(bars + C::q_full + 8 * x, 1);
+            mbar_init(bars + C::q_empty + 8 * x, 1);
+        }
+        mbar_init(bars + C::ex_full, 8);
+        mbar_init(bars + C::ex_free, 8);
+        mbar_init(bars + C::mma_drained, 1);
+        mbar_fence_init();
+        s_abort[0] = 0;
+        s_abort[1] = (int)p.wait_limit_ns;
+        for (int s = 0; s < C::kSlots + 2 + C::kRaw; ++s) s_armed[s] = -1;
+    }
+    if (warp == 0) {
+        tmem_alloc(bars + C::tmem_slot, 512);
+        tmem_relinquish();
+    }
+    pdl_trigger();
+    pdl_wait();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + C::kOffBar + C::tmem_slot);
+    auto wait_all = [](uint32_t bar, uint32_t parity, volatile int* abort_flag) { return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag)); };
+
+    constexpr uint32_t kColO = 256;
+    const int share0 = share_begin(p.units, blockIdx.x, gridDim.x), share1 = share_begin(p.units, blockIdx.x + 1, gridDim.x);
+    PieceIter<Rows> iter(rows, p.n, p.G, share0, share1);
+    Piece it;
+    const int tile_tok = kRows / p.G, g_shift = 31 - __clz(p.G);
+
+    if (warp < 8) {
+        // ====================================================================
+        // softmax
+        // ====================================================================
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+        const int x = warp >> 2, t = threadIdx.x & 127;
+        const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t s_addr = tmem + lane_addr + x * 128;
+        constexpr float kScaleLog2 = scale_log2(D);
+        uint32_t g = 0, steps_x = 0, items_x = 0, n_item = 0, n_ex = 0;  // steps of all items; of this stream: steps and items with any; items; exchanges
+        bool ok = true, must_wait_free = false;
+        while (ok && iter.next(it)) {
+            const int n_x = it.n_x(p.G), n_tiles = it.tile1 - it.tile0, n_steps = n_tiles * n_x;
+            const int first = (int)((x - g) & 1);                    // this stream's first step of the item
+            const int q_tile = n_x == 2 ? first : 0;
+            const int row_tok = q_tile * tile_tok + (t >> g_shift);  // token of this row within the item
+            const bool valid = row_tok < it.n_tok;
+            const bool warp_valid = q_tile * tile_tok + (((t & ~31)) >> g_shift) < it.n_tok;  // any row of this warp
+            const int64_t token = it.q_tok + row_tok;
+            const uint32_t* const mask_row = p.mask + token * 2 * p.mask_words;
+            float m = -INFINITY, l = 0.f, lu = 0.f;  // running maximum (log2 units), sums of the rounded and of the exact weights
+            int mine = 0;
+            for (int s = first; s < n_steps; s += 2, ++mine) {
+                ok = wait_all(bars + C::s_full + 8 * x, steps_x & 1, s_abort);
+                if (!ok) break;
+                ++steps_x;
+                tc_fence_after();
+                if (warp_valid) {
+                    const int key0 = (it.tile0 + (n_x == 2 ? s >> 1 : s)) * kTileKeys;
+                    const bool masked = key0 + kTileKeys > it.prior;
+                    uint32_t sv[4][32];
+                    tmem_ld32(s_addr, sv[0]);
+                    tmem_ld32(s_addr + 32, sv[1]);
+                    tmem_ld32(s_addr + 64, sv[2]);
+                    tmem_ld32(s_addr + 96, sv[3]);
+                    uint32_t vis[4];
+                    if (masked) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) vis[q] = valid ? mask_bits(mask_row, key0 + 32 * q - it.prior, it.nodes) : 0u;
+                    }
+                    tmem_wait_ld();
+                    if (masked) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+#pragma unroll
+                            for (int c = 0; c < 32; ++c)
+                                if (!(vis[q] >> c & 1u)) sv[q][c] = 0xff800000u;
+                    }
+                    float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int c = 0; c < 32; c += 8) {
+                            mx0 = max3(mx0, __uint_as_float(sv[q][c]), __uint_as_float(sv[q][c + 1]));
+                            mx1 = max3(mx1, __uint_as_float(sv[q][c + 2]), __uint_as_float(sv[q][c + 3]));
+                            mx2 = max3(mx2, __uint_as_float(sv[q][c + 4]), __uint_as_float(sv[q][c + 5]));
+                            mx3 = max3(mx3, __uint_as_float(sv[q][c + 6]), __uint_as_float(sv[q][c + 7]));
+                        }
+                    const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * kScaleLog2;
+                    const float m_new = mx > m + kRescaleThreshold ? mx : m;  // also the first finite maximum
+                    const float alpha = m_new == m ? 1.f : fast_exp2(m - m_new);
+                    // (the commit that raised s_full came after this stream's last PV)
+                    if (mine > 0 && __any_sync(0xffffffffu, m_new != m)) {
+                        const uint32_t o_addr = tmem + lane_addr + kColO + x * D;
+#pragma unroll 1
+                        for (int c0 = 0; c0 < D; c0 += 32) {
+                            uint32_t v[32];
+                            tmem_ld32(o_addr + c0, v);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(__uint_as_float(v[c]) * alpha);
+                            tmem_st32(o_addr + c0, v);
+                        }
+                        tmem_wait_st();
+                    }
+                    l *= alpha;
+                    lu *= alpha;
+                    m = m_new;
+                    const float m_sub = m == -INFINITY ? 0.f : m;
+                    const uint64_t sc2 = pack2(kScaleLog2, kScaleLog2), nm2 = pack2(-m_sub, -m_sub);
+                    // (masked scores are -inf, and their weights exp2(-inf) = 0)
+                    uint64_t ls0 = 0ull, ls1 = 0ull;
+                    float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+                    for (int hhalf = 0; hhalf < 2; ++hhalf) {
+                        uint32_t packed[32];
+#pragma unroll
+                        for (int qq = 0; qq < 2; ++qq) {
+                            const int q = hhalf * 2 + qq;
+#pragma unroll
+                            for (int c = 0; c < 32; c += 2) {
+                                float e0, e1;
+                                unpack2(fma2(pack2(__uint_as_float(sv[q][c]), __uint_as_float(sv[q][c + 1])), sc2, nm2), e0, e1);
+                                e0 = fast_exp2(e0), e1 = fast_exp2(e1);
+                                if (c & 2) ls1 = add2(ls1, pack2(e0, e1));
+                                else ls0 = add2(ls0, pack2(e0, e1));
+                                packed[qq * 16 + (c >> 1)] = pack_bf16(e0, e1);
+                                if (masked) {
+                                    // (rows of few keys: the sum of the weights that PV multiplies keeps the output an exact mix of V rows)
+                                    l0 += bf16_lo(packed[qq * 16 + (c >> 1)]);
+                                    l1 += bf16_hi(packed[qq * 16 + (c >> 1)]);
+                                }
+                            }
+                        }
+                        tmem_st32(s_addr + hhalf * 32, packed);
+                    }
+                    float a0, a1, a2, a3;
+                    unpack2(ls0, a0, a1);
+                    unpack2(ls1, a2, a3);
+                    const float sum = (a0 + a2) + (a1 + a3);
+                    lu += sum;
+                    l += masked ? l0 + l1 : sum;
+                    tmem_wait_st();
+                }
+                if (must_wait_free) {
+                    // the other stream's warps have read this stream's last accumulator, which the product to come overwrites
+                    ok = wait_all(bars + C::ex_free, (n_ex & 1) ^ 1, s_abort);
+                    if (!ok) break;
+                    must_wait_free = false;
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bars + C::p_ready + 8 * x);
+            }
+            if (!ok) break;
+            // ---- the item's end ----
+            if (mine > 0) {
+                ok = wait_all(bars + C::o_done + 8 * x, items_x & 1, s_abort);
+                if (!ok) break;
+                ++items_x;
+                tc_fence_after();
+            }
+            float w0 = 1.f, w1 = 0.f;  // weights of the accumulators (streams 0 and 1 where both have a part of the row)
+            int col0 = 0, col1 = D;
+            uint32_t o0 = tmem + lane_addr + kColO + x * D, o1 = o0;
+            bool both = false;
+            if (n_x == 1) {
+                // rows of one q tile: join the streams; each writes half of the columns
+                if (must_wait_free) {
+                    ok = wait_all(bars + C::ex_free, (n_ex & 1) ^ 1, s_abort);
+                    if (!ok) break;
+                    must_wait_free = false;
+                }
+                exchange[x * kRows + t] = make_float2(m, lu);
+                rounding[x * kRows + t] = __float2half_rn(lu > 0.f ? (l - lu) / lu : 0.f);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bars + C::ex_full);
+                ok = wait_all(bars + C::ex_full, n_ex & 1, s_abort);
+                if (!ok) break;
+                tc_fence_after();
+                const float2 a = exchange[t], b = exchange[kRows + t];
+                const float ra = 1.f + __half2float(rounding[t]), rb = 1.f + __half2float(rounding[kRows + t]);
+                ++n_ex;
+                must_wait_free = true;
+                const bool has0 = n_steps > 1 || (g & 1) == 0, has1 = n_steps > 1 || (g & 1) == 1;
+                both = has0 && has1;
+                m = fmaxf(has0 ? a.x : -INFINITY, has1 ? b.x : -INFINITY);
+                const float m_sub = m == -INFINITY ? 0.f : m;
+                w0 = has0 ? fast_exp2(a.x - m_sub) : 0.f;
+                w1 = has1 ? fast_exp2(b.x - m_sub) : 0.f;
+                const float lu0 = has0 ? a.y * w0 : 0.f, lu1 = has1 ? b.y * w1 : 0.f;
+                lu = lu0 + lu1;
+                l = lu0 * ra + lu1 * rb;
+                o0 = tmem + lane_addr + kColO;
+                o1 = o0 + D;
+                if (!has0) o0 = o1, w0 = w1;
+                col0 = x * (D / 2);
+                col1 = col0 + D / 2;
+            }
+            if (warp_valid) {
+                const bool whole = it.whole();
+                const float inv = !whole ? 1.f : l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;  // (l NaN: a score was)
+                const int head = it.head * p.G + (t & (p.G - 1));
+                const int slot_row = (2 * (int)blockIdx.x + (it.tile0 > 0 ? 0 : 1)) * kGroupRows + q_tile * kRows + t;
+                uint32_t flags = 0;
+                if (it.kv_len > it.tile0 * kTileKeys && it.tile1 > it.tree_tile()) {
+#pragma unroll
+                    for (int w = 0; w < kMaxNodes / 32; ++w) flags |= s_flagged[(n_item % C::kFlagRing) * 8 + w];
+                }
+#pragma unroll 1
+                for (int c0 = col0; c0 < col1; c0 += 32) {
+                    uint32_t v[32];
+                    tmem_ld32(o0 + c0, v);
+                    if (both) {
+                        uint32_t u[32];
+                        tmem_ld32(o1 + c0, u);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(fmaf(__uint_as_float(v[c]), w0, __uint_as_float(u[c]) * w1));
+                    } else {
+                        tmem_wait_ld();
+                        if (n_x == 1) {
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(__uint_as_float(v[c]) * w0);
+                        }
+                    }
+                    if (flags && valid) {
+                        // tree tokens whose V row was taken out of the products: their weight times that row
+#pragma unroll 1
+                        for (int w = 0; w < kMaxNodes / 32; ++w) {
+                            uint32_t todo = s_flagged[(n_item % C::kFlagRing) * 8 + w] & mask_word(mask_row, min(w, 2 * p.mask_words - 1), 32 * w < it.nodes ? it.nodes : 0);
+                            while (todo) {
+                                const int pos = it.prior + 32 * w + __ffs(todo) - 1;
+                                todo &= todo - 1;
+                                const int64_t page = __ldg(p.block_table + (int64_t)it.r * p.max_pages + pos / kPage);
+                                const char* const blk = p.pool + (page * p.Hkv + it.head) * (int64_t)page_head_bytes(D);
+                                const __nv_bfloat16* const qr = p.q + (token * p.Hq + head) * D;
+                                float dot = 0.f;
+#pragma unroll 1
+                                for (int e = 0; e < D; ++e)
+                                    dot = fmaf(__bfloat162float(qr[e]), __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(blk + unit_offset(pos % kPage, e) + 2 * (e & 7))), dot);
+                                const float weight = fast_exp2(fmaf(dot, kScaleLog2, -m));
+                                const char* const vrow = blk + block_bytes(D);
+#pragma unroll
+                                for (int c = 0; c < 32; ++c)
+                                    v[c] = __float_as_uint(fmaf(weight, __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(vrow + unit_offset(pos % kPage, c0 + c) + 2 * (c & 7))), __uint_as_float(v[c])));
+                            }
+                        }
+                    }
+                    if (valid) {
+                        if (whole) {
+                            uint32_t y[16];
+#pragma unroll
+                            for (int c = 0; c < 32; c += 2) y[c / 2] = pack_bf16(__uint_as_float(v[c]) * inv, __uint_as_float(v[c + 1]) * inv);
+                            uint4* const dst = reinterpret_cast<uint4*>(p.out + (token * p.Hq + head) * D + c0);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) dst[k] = make_uint4(y[4 * k], y[4 * k + 1], y[4 * k + 2], y[4 * k + 3]);
+                        } else {
+                            uint4* const dst = reinterpret_cast<uint4*>(p.part_o + (int64_t)slot_row * D + c0);
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) dst[k] = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                        }
+                    }
+                }
+                if (valid && col0 == 0) {
+                    if (!whole) p.part_ml[slot_row] = make_float4(m, l, lu, 0.f);
+                    else if (p.lse) p.lse[token * p.Hq + head] = lu > 0.f ? (m + log2f(lu)) * 0.6931471805599453f : lu == 0.f ? -INFINITY : lu;
+                }
+            }
+            if (n_x == 1) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bars + C::ex_free);
+            }
+            g += n_steps;
+            ++n_item;
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
+        if (warp == kLoadWarp) {
+            // ================================================================
+            // K and V tiles, in the order of use; entry e of the ring lies in slot e % kSlots
+            // ================================================================
+            const uint64_t policy = l2_policy_evict_first();
+            int j = 0, head = 0;
+            const int32_t* bt = nullptr;
+            it.tile1 = 0;
+            bool have = true, ok = true;
+            // page of the next tile (lanes 0-7), requested a tile ahead of its use; -1: none, -2: the sequence has ended there
+            auto fetch = [&](int& page, int& kv_head, bool& tree) {
+                if (j == it.tile1) {
+                    have = iter.next(it);
+                    if (!have) return;
+                    j = it.tile0;
+                    head = it.head;
+                    bt = p.block_table + (int64_t)it.r * p.max_pages;
+                }
+                const int at = j * (kTileKeys / kPage) + lane;
+                page = lane < kTileKeys / kPage && at * kPage < it.kv_len ? __ldg(bt + at) : -2;
+                kv_head = head;
+                tree = j >= it.tree_tile();
+                ++j;
+            };
+            auto pool_row = [&](int page, int kv_head) {
+                const bool good = (uint32_t)page < (uint64_t)p.num_pages;
+                if (!good && page != -2 && lane < kTileKeys / kPage) atomicOr(p.flag, kStatusBounds);
+                return good ? (page * p.Hkv + kv_head) * (2 * C::kHalves) : -8;  // (rows outside the pool read as zero)
+            };
+            uint32_t n_raw = 0;
+            auto load = [&](int row, uint32_t e, int block, bool raw) {
+                int r[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    r[k] = __shfl_sync(0xffffffffu, row, k);
+                    r[k] = r[k] < 0 ? r[k] : r[k] + block;
+                }
+                const uint32_t s = e % C::kSlots, par = (e / C::kSlots) & 1;
+                if (!wait_all(bars + C::empty + 8 * s, par ^ 1, s_abort)) return false;
+                if (elect_one()) {
+                    const uint32_t land = bars + (raw ? C::raw + 8 * (n_raw % C::kRaw) : C::full + 8 * s), dst = sbase + C::kOffKV + s * C::kTileBytes;
+                    mbar_expect_tx(land, C::kTileBytes);
+                    if (raw) s_armed[C::kSlots + 2 + n_raw % C::kRaw] = (int)(n_raw / C::kRaw & 1);
+                    else s_armed[s] = (int)par;
+#pragma unroll
+                    for (int h = 0; h < C::kHalves; ++h) {
+                        gather4(dst + h * C::kHalfBytes, &pool_map, r[0] + (r[0] < 0 ? 0 : h), r[1] + (r[1] < 0 ? 0 : h), r[2] + (r[2] < 0 ? 0 : h), r[3] + (r[3] < 0 ? 0 : h), land, policy);
+                        gather4(dst + h * C::kHalfBytes + 4 * kPoolBlock, &pool_map, r[4] + (r[4] < 0 ? 0 : h), r[5] + (r[5] < 0 ? 0 : h), r[6] + (r[6] < 0 ? 0 : h), r[7] + (r[7] < 0 ? 0 : h), land, policy);
+                    }
+                }
+                __syncwarp();
+                return true;
+            };
+            int page = -2, kv_head = 0;
+            bool tree = false;
+            fetch(page, kv_head, tree);
+            if (have) {
+                int row = pool_row(page, kv_head);
+                bool tree_v = tree;
+                fetch(page, kv_head, tree);
+                ok = load(row, 0, 0, false);
+                for (uint32_t n = 0; ok; ++n) {  // K of tile n + 1, V of tile n
+                    const int row_v = row;
+                    const bool more = have, raw = tree_v;
+                    if (more) {
+                        row = pool_row(page, kv_head);
+                        tree_v = tree;
+                        fetch(page, kv_head, tree);
+                        ok = load(row, 2 * n + 1, 0, false);
+                        if (!ok) break;
+                    }
+                    ok = load(row_v, 2 * n + 2, C::kHalves, raw);
+                    if (raw) ++n_raw;
+                    if (!more) break;
+                }
+            }
+        } else if (warp == kMmaWarp) {
+            // ================================================================
+            // MMA issue: QK^T of step i + 2 behind PV of step i, across items
+            // ================================================================
+            constexpr uint32_t kIdescQK = instr_desc(kRows, kTileKeys, false), kIdescPV = instr_desc(kRows, D, true);
+            const uint64_t desc_kmajor = smem_desc(0, 16, 1024), desc_v = smem_desc(0, C::kHalfBytes, 1024);
+            PieceIter<Rows> iter_v = iter;
+            Piece iv;
+            bool ok = true;
+            uint32_t k_tile = 0, v_tile = 0;         // tiles that QK^T and PV have finished
+            uint32_t gk = 0, gv = 0;                 // steps that they have issued
+            uint32_t q_tiles = 0;                    // q tiles of the items before QK^T's
+            int sk = 0, nk = 0, xk = 1, sv = 0, nv = 0, xv = 1;  // step within the item, its steps, its q tiles
+            bool have_k = true;
+            while (ok) {
+                if (have_k && gk - gv < 2) {
+                    if (sk == nk) {
+                        if (nk > 0) q_tiles += xk;
+                        have_k = iter.next(it);
+                        if (!have_k) continue;
+                        xk = it.n_x(p.G);
+                        nk = (it.tile1 - it.tile0) * xk;
+                        sk = 0;
+                    }
+                    const int qt = xk == 2 ? sk & 1 : 0;
+                    const bool tile_ends = xk == 1 || qt == 1;
+                    const uint32_t e = k_tile == 0 ? 0 : 2 * k_tile - 1, s = e % C::kSlots, qn = q_tiles + qt, qs = qn & 1;
+                    if (sk < xk) {
+                        ok = wait_all(bars + C::q_full + 8 * qs, (qn >> 1) & 1, s_abort);
+                        if (!ok) break;
+                    }
+                    if (qt == 0) {
+                        ok = wait_all(bars + C::full + 8 * s, (e / C::kSlots) & 1, s_abort);
+                        if (!ok) break;
+                    }
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint64_t qd = desc_kmajor + ((sbase + C::kOffQ + qs * C::kTileBytes) >> 4), kd = desc_kmajor + ((sbase + C::kOffKV + s * C::kTileBytes) >> 4);
+#pragma unroll
+                        for (int kk = 0; kk < D / 16; ++kk) {
+                            const uint32_t off = ((kk >> 2) * C::kHalfBytes + (kk & 3) * 32) >> 4;
+                            tc_mma_ss(tmem + (gk & 1) * 128, qd + off, kd + off, kIdescQK, kk > 0);
+                        }
+                        tc_commit(bars + C::s_full + 8 * (gk & 1));
+                        if (tile_ends) tc_commit(bars + C::empty + 8 * s);
+                        if (sk + xk >= nk) tc_commit(bars + C::q_empty + 8 * qs);
+                    }
+                    __syncwarp();
+                    if (tile_ends) ++k_tile;
+                    ++sk;
+                    ++gk;
+                    continue;
+                }
+                if (gv == gk) break;
+                if (sv == nv) {
+                    iter_v.next(iv);
+                    xv = iv.n_x(p.G);
+                    nv = (iv.tile1 - iv.tile0) * xv;
+                    sv = 0;
+                }
+                const bool tile_begins = xv == 1 || (sv & 1) == 0, tile_ends = xv == 1 || (sv & 1) == 1;
+                const uint32_t e = 2 * v_tile + 2, s = e % C::kSlots, x = gv & 1;
+                if (tile_begins) {
+                    ok = wait_all(bars + C::full + 8 * s, (e / C::kSlots) & 1, s_abort);
+                    if (!ok) break;
+                }
+                ok = wait_all(bars + C::p_ready + 8 * x, (gv >> 1) & 1, s_abort);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t vd = desc_v + ((sbase + C::kOffKV + s * C::kTileBytes) >> 4);
+#pragma unroll
+                    for (int kk = 0; kk < kTileKeys / 16; ++kk)
+                        tc_mma_ts(tmem + kColO + x * D, tmem + x * 128 + kk * 8, vd + kk * (2048 >> 4), kIdescPV, (sv >= 2 || kk > 0) ? 1u : 0u);
+                    if (tile_ends) tc_commit(bars + C::empty + 8 * s);
+                    if (sv + 2 >= nv) tc_commit(bars + C::o_done + 8 * x);
+                }
+                __syncwarp();
+                if (tile_ends) ++v_tile;
+                ++sv;
+                ++gv;
+            }
+        } else if (warp == kQWarp) {
+            // ================================================================
+            // Q tiles: rows (token, head of the group) in token-major order, a box of [128 / G tokens][G heads][64 elements] per half
+            // ================================================================
+            uint32_t n = 0;
+            bool ok = true;
+            while (ok && iter.next(it)) {
+                for (int x = 0; x < it.n_x(p.G) && ok; ++x, ++n) {
+                    ok = wait_all(bars + C::q_empty + 8 * (n & 1), ((n >> 1) & 1) ^ 1, s_abort);
+                    if (ok && elect_one()) {
+                        mbar_expect_tx(bars + C::q_full + 8 * (n & 1), C::kTileBytes);
+                        s_armed[C::kSlots + (n & 1)] = (int)((n >> 1) & 1);
+#pragma unroll
+                        for (int h = 0; h < C::kHalves; ++h)
+                            tma_load_3d(sbase + C::kOffQ + (n & 1) * C::kTileBytes + h * C::kHalfBytes, &q_map, h * 64, it.head * p.G, it.q_tok + x * tile_tok, bars + C::q_full + 8 * (n & 1));
+                    }
+                    __syncwarp();
+                }
+            }
+        } else {
+            // ================================================================
+            // V rows that no product may read
+            // ================================================================
+            // (they land on barriers of their own, and this warp's arrival takes the place of the copy's on the slot's)
+            uint32_t v_tile = 0, n_item = 0, n_raw = 0;
+            bool ok = true;
+            while (ok && iter.next(it)) {
+                volatile uint32_t* const flagged = s_flagged + (n_item % C::kFlagRing) * 8;
+                if (lane < 8) flagged[lane] = 0u;
+                __syncwarp();
+                for (int j = it.tile0; j < it.tile1 && ok; ++j, ++v_tile) {
+                    if (j < it.tree_tile()) continue;
+                    const uint32_t s = (2 * v_tile + 2) % C::kSlots;
+                    ok = wait_all(bars + C::raw + 8 * (n_raw % C::kRaw), n_raw / C::kRaw & 1, s_abort);
+                    if (!ok) break;
+                    ++n_raw;
+                    for (int q = 0; q < 4; ++q) {
+                        const int key = j * kTileKeys + 32 * q + lane;
+                        char* const row = smem + C::kOffKV + s * C::kTileBytes + (32 * q + lane) * 128;
+                        bool clear = key >= it.kv_len;
+                        if (key >= it.prior && !clear) {
+#pragma unroll
+                            for (int h = 0; h < C::kHalves; ++h)
+#pragma unroll
+                                for (int u = 0; u < 8; ++u)
+                                    clear = any_not_finite(*reinterpret_cast<const uint4*>(row + h * C::kHalfBytes + ((u ^ (lane & 7)) << 4))) || clear;
+                            if (clear) atomicOr(const_cast<uint32_t*>(flagged) + ((key - it.prior) >> 5), 1u << ((key - it.prior) & 31));
+                        }
+                        if (clear) {
+#pragma unroll
+                            for (int h = 0; h < C::kHalves; ++h)
+#pragma unroll
+                                for (int u = 0; u < 8; ++u) *reinterpret_cast<uint4*>(row + h * C::kHalfBytes + ((u ^ (lane & 7)) << 4)) = make_uint4(0, 0, 0, 0);
+                        }
+                    }
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bars + C::full + 8 * s);
+                }
+                ++n_item;
+            }
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();  // every role has left its loop
+    if (*s_abort) {
+        // A bounded wait ran out: the output is invalid and the pool is flagged.  Copies under way get a bounded time to land, the MMAs
+        // issued so far to retire, before shared and tensor memory are given back.
+        if (threadIdx.x == 0) atomicOr(p.flag, kStatusTimeout);
+        if (warp == kLoadWarp) {
+            for (int s = 0; s < C::kSlots; ++s)
+                if (s_armed[s] >= 0) mbar_wait(bars + C::full + 8 * s, (uint32_t)s_armed[s], kDrainLimitNs);
+            for (int k = 0; k < C::kRaw; ++k)
+                if (s_armed[C::kSlots + 2 + k] >= 0) mbar_wait(bars + C::raw + 8 * k, (uint32_t)s_armed[C::kSlots + 2 + k], kDrainLimitNs);
+            for (int x = 0; x < 2; ++x)
+                if (s_armed[C::kSlots + x] >= 0) mbar_wait(bars + C::q_full + 8 * x, (uint32_t)s_armed[C::kSlots + x], kDrainLimitNs);
+        }
+        if (warp == kMmaWarp) {
+            if (elect_one()) tc_commit(bars + C::mma_drained);
+            __syncwarp();
+            mbar_wait(bars + C::mma_drained, 0, kDrainLimitNs);
+        }
+        tc_fence_before();
+        __syncthreads();
+    }
+    if (warp == 0) tmem_dealloc(tmem, 512);
+}
+
+// ---------------------------------------------------------------------------
+// Items that a share's border cuts: with M the largest of the pieces' maxima,
+//     out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s,
+// piece after piece in the order of their keys.  blockIdx.x + 1 is the share that begins inside the item and is the first to; a warp
+// has four rows.
+// ---------------------------------------------------------------------------
+constexpr int kMergeThreads = 256, kMergeRows = 4;  // rows of a warp
+
+template <int D, class Rows>
+__global__ void __launch_bounds__(kMergeThreads) tree_merge_kernel(const __grid_constant__ TreeParams p, int n_cta, const __grid_constant__ Rows rows) {
+    constexpr int V = D / 32;
+    pdl_trigger();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int c = (int)blockIdx.x + 1, border = share_begin(p.units, c, n_cta);
+    int r;
+    {
+        int lo = 0, hi = p.n - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (rows.unit_start[mid] <= border) lo = mid; else hi = mid - 1;
+        }
+        r = lo;
+    }
+    const int prior = rows.prior[r], q_tok = rows.q_start[r], nodes = rows.q_start[r + 1] - q_tok;
+    const int tiles = (prior + nodes + kTileKeys - 1) / kTileKeys, per = tiles + kItemUnits;
+    const int item = (border - rows.unit_start[r]) / per, begin = rows.unit_start[r] + item * per, end = begin + per;
+    pdl_wait();
+    // (a border at an item's begin cuts nothing, nor does one before its first tile; and the item is the first border's inside it)
+    const int first_tile = begin + kItemUnits;
+    if (border <= first_tile || share_begin(p.units, c - 1, n_cta) > first_tile) return;
+    const int group_tok = kGroupRows / p.G, groups = (nodes + group_tok - 1) / group_tok;
+    const int head = item / groups, tok0 = (item - head * groups) * group_tok, n_rows = min(group_tok, nodes - tok0) * p.G;
+    const int row0 = ((int)blockIdx.y * (kMergeThreads / 32) + warp) * kMergeRows;
+    if (row0 >= n_rows) return;
+    // pieces: shares c - 1, c, ...: the first one's begins with the item, so it lies in its share's second place, the others' in the first
+    int n_seg = 2;
+    while (share_begin(p.units, c + n_seg - 1, n_cta) < end) ++n_seg;
+    auto place = [&](int s) { return (int64_t)(2 * (c - 1 + s) + (s == 0 ? 1 : 0)) * kGroupRows; };
+    float M[kMergeRows], l[kMergeRows], lu[kMergeRows], acc[kMergeRows][V];
+#pragma unroll
+    for (int k = 0; k < kMergeRows; ++k) {
+        M[k] = -INFINITY, l[k] = lu[k] = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) acc[k][v] = 0.f;
+    }
+    for (int s = 0; s < n_seg; ++s) {
+        float4 ml[kMergeRows];
+        float x[kMergeRows][V];
+#pragma unroll
+        for (int k = 0; k < kMergeRows; ++k) {
+            const int64_t at = place(s) + min(row0 + k, n_rows - 1);
+            ml[k] = p.part_ml[at];
+            const float* const src = p.part_o + at * D + lane * V;
+            if (V == 4) *reinterpret_cast<float4*>(x[k]) = *reinterpret_cast<const float4*>(src);
+            else *reinterpret_cast<float2*>(x[k]) = *reinterpret_cast<const float2*>(src);
+        }
+#pragma unroll
+        for (int k = 0; k < kMergeRows; ++k) {
+            const float top = fmaxf(M[k], ml[k].x), base = top == -INFINITY ? 0.f : top;
+            const float a = fast_exp2(M[k] - base), b = fast_exp2(ml[k].x - base);
+            M[k] = top;
+            l[k] = fmaf(l[k], a, ml[k].y * b);
+            lu[k] = fmaf(lu[k], a, ml[k].z * b);
+#pragma unroll
+            for (int v = 0; v < V; ++v) acc[k][v] = fmaf(acc[k][v], a, x[k][v] * b);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kMergeRows; ++k) {
+        const int row = row0 + k;
+        if (row >= n_rows) break;
+        const float inv = l[k] > 0.f ? 1.f / l[k] : l[k] == 0.f ? 0.f : l[k];
+        const int64_t at = (int64_t)(q_tok + tok0 + row / p.G) * p.Hq + head * p.G + row % p.G;
+        uint32_t* const dst = reinterpret_cast<uint32_t*>(p.out + at * D + lane * V);
+#pragma unroll
+        for (int v = 0; v < V; v += 2) dst[v / 2] = pack_bf16(acc[k][v] * inv, acc[k][v + 1] * inv);
+        if (p.lse && lane == 0) p.lse[at] = lu[k] > 0.f ? (M[k] + log2f(lu[k])) * 0.6931471805599453f : lu[k] == 0.f ? -INFINITY : lu[k];
+    }
+}
+
+constexpr int kSms = 148;  // of the device that the library is built for: CTAs, and places in the workspace
+
+size_t workspace_bytes(const ps_shape& s) { return 2 * (size_t)kSms * kGroupRows * (s.head_dim * sizeof(float) + sizeof(float4)); }
+
+struct TreeCall {
+    const KvPool* pool;
+    const void* q;
+    const int32_t* block_table;
+    int32_t max_pages;
+    const int64_t* mask;
+    int32_t mask_words;
+    const int32_t *prior, *n_nodes;
+    int32_t n;
+    void* out;
+    float* lse;
+    char* ws;
+    cudaStream_t stream;
+};
+
+template <int D, int N>
+ps_status launch_rows(const TreeCall& a) {
+    const ps_shape& shape = a.pool->shape;
+    const int Hq = shape.n_q_heads, Hkv = shape.n_kv_heads, G = Hq / Hkv, group_tok = kGroupRows / G;
+    using Rows = TreeRows<N>;
+    Rows rows;  // (entries past n are not read)
+    int64_t units = 0;
+    int32_t tokens = 0;
+    bool wide = false;
+    for (int r = 0; r < a.n; ++r) {
+        rows.q_start[r] = tokens;
+        rows.unit_start[r] = (int32_t)units;
+        rows.prior[r] = a.prior[r];
+        tokens += a.n_nodes[r];
+        const int groups = (a.n_nodes[r] + group_tok - 1) / group_tok;
+        wide = wide || groups > 1;
+        units += (int64_t)Hkv * groups * (((int64_t)a.prior[r] + a.n_nodes[r] + kTileKeys - 1) / kTileKeys + kItemUnits);
+        if (units > 0x3fffffff) return fail(PS_ERR_INVALID, "too many keys in one batch");
+    }
+    rows.q_start[a.n] = tokens;
+    rows.unit_start[a.n] = (int32_t)units;
+
+    static PerDeviceOnce configured;
+    const ps_status cfg = once_per_device(configured, []() -> ps_status {
+        PS_CUDA_TRY(cudaFuncSetAttribute(tree_kernel<D, Rows>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::kSmemBytes));
+        return PS_OK;
+    });
+    if (cfg != PS_OK) return cfg;
+    RunArgs m{};
+    m.shape = shape;
+    m.pool = a.pool->base;
+    m.num_pages = a.pool->num_pages;
+    m.q = (const __nv_bfloat16*)a.q;
+    m.total_q = tokens;
+    CUtensorMap q_map, pool_map;
+    ps_status st = encode_q_map(m, &q_map);
+    if (st == PS_OK) st = encode_pool_map(m, &pool_map);
+    if (st != PS_OK) return st;
+    TreeParams p{};
+    p.q = m.q;
+    p.block_table = a.block_table;
+    p.mask = (const uint32_t*)a.mask;
+    p.pool = a.pool->base;
+    p.out = (__nv_bfloat16*)a.out;
+    p.lse = a.lse;
+    p.part_ml = (float4*)a.ws;
+    p.part_o = (float*)(a.ws + 2 * (size_t)kSms * kGroupRows * sizeof(float4));
+    p.flag = a.pool->flag_dev;
+    p.num_pages = a.pool->num_pages;
+    p.wait_limit_ns = (uint32_t)a.pool->wait_limit_ns;
+    p.max_pages = a.max_pages, p.mask_words = a.mask_words, p.n = a.n, p.Hq = Hq, p.Hkv = Hkv, p.G = G, p.units = (int32_t)units;
+    const int grid = (int)(units / 2 < kSms ? units / 2 : kSms);  // (an item has at least two units: no share is empty)
+    st = launch_kernel(tree_kernel<D, Rows>, grid, kThreads, Cfg<D>::kSmemBytes, a.stream, 1, true, p, q_map, pool_map, rows);
+    if (st != PS_OK || grid == 1) return st;
+    return launch_kernel(tree_merge_kernel<D, Rows>, dim3(grid - 1, kGroupRows / (kMergeThreads / 32 * kMergeRows)), kMergeThreads, 0, a.stream, 1, true, p, grid, rows);
+}
+
+}  // namespace
+
+}  // namespace ps
+
+using namespace ps;
+
+extern "C" {
+
+ps_status ps_attn_tree_workspace(const ps_shape* shape, size_t* bytes_out) {
+    const ps_status st = check_shape(shape);
+    if (st != PS_OK) return st;
+    if (!bytes_out) return fail(PS_ERR_INVALID, "null argument");
+    *bytes_out = workspace_bytes(*shape);
+    return PS_OK;
+}
+
+ps_status ps_attn_tree(const ps_kv* kv, const void* q_dev, const int32_t* block_table_dev, int32_t max_pages, const int64_t* mask_dev, int32_t mask_words,
+                       const int32_t* prior_host, const int32_t* n_nodes_host, int32_t n, void* out_dev, float* lse_out_dev, void* workspace_dev,
+                       size_t workspace_bytes_given, void* stream) {
+    if (!kv || !q_dev || !block_table_dev || !mask_dev || !prior_host || !n_nodes_host || !out_dev || !workspace_dev) return fail(PS_ERR_INVALID, "null argument");
+    if (n < 1 || max_pages < 1) return fail(PS_ERR_INVALID, "n=%d, max_pages=%d must be positive", n, max_pages);
+    if (mask_words < 1 || mask_words > kMaxNodes / 64) return fail(PS_ERR_UNSUPPORTED, "mask_words=%d: masks of 1 to %d words are supported", mask_words, kMaxNodes / 64);
+    const KvPool& pool = pool_of(kv);
+    if (pool.shape.dtype != 0) return fail(PS_ERR_UNSUPPORTED, "tree attention is supported on bf16 pools only");
+    if (workspace_bytes_given < workspace_bytes(pool.shape))
+        return fail(PS_ERR_WORKSPACE, "workspace has %zu bytes, tree attention needs %zu", workspace_bytes_given, workspace_bytes(pool.shape));
+    if ((uintptr_t)workspace_dev % 256 != 0) return fail(PS_ERR_INVALID, "workspace must be 256-byte aligned");
+    if (((uintptr_t)q_dev | (uintptr_t)out_dev) % 16 != 0) return fail(PS_ERR_INVALID, "q and out must be 16-byte aligned");
+    int64_t T = 0;
+    for (int r = 0; r < n; ++r) {
+        if (prior_host[r] < 0 || n_nodes_host[r] < 1) return fail(PS_ERR_INVALID, "request %d: %d nodes behind %d tokens", r, n_nodes_host[r], prior_host[r]);
+        if (n_nodes_host[r] > 64 * mask_words) return fail(PS_ERR_INVALID, "request %d: %d nodes in a mask of %d bits", r, n_nodes_host[r], 64 * mask_words);
+        if ((int64_t)prior_host[r] + n_nodes_host[r] > (int64_t)max_pages * kPage) return fail(PS_ERR_INVALID, "request %d: its tokens exceed max_pages * page_size", r);
+        T += n_nodes_host[r];
+        if (T > (1 << 24)) return fail(PS_ERR_INVALID, "more than 2^24 tokens in one batch");
+    }
+    const int64_t row = (int64_t)pool.shape.n_q_heads * pool.shape.head_dim;
+    int64_t t0 = 0;
+    for (int32_t r0 = 0; r0 < n; r0 += kTreeRowsMax) {  // (a slice's kernel waits for the one before, whose workspace it uses)
+        const int32_t m = n - r0 < kTreeRowsMax ? n - r0 : kTreeRowsMax;
+        const TreeCall a{&pool, (const char*)q_dev + t0 * row * 2, block_table_dev + (int64_t)r0 * max_pages, max_pages, mask_dev + t0 * mask_words, mask_words, prior_host + r0,
+                         n_nodes_host + r0, m, (char*)out_dev + t0 * row * 2, lse_out_dev ? lse_out_dev + t0 * pool.shape.n_q_heads : nullptr, (char*)workspace_dev,
+                         (cudaStream_t)stream};
+        const ps_status st = pool.shape.head_dim == 128 ? (m <= 64 ? launch_rows<128, 64>(a) : m <= 512 ? launch_rows<128, 512>(a) : launch_rows<128, kTreeRowsMax>(a))
+                                                        : (m <= 64 ? launch_rows<64, 64>(a) : m <= 512 ? launch_rows<64, 512>(a) : launch_rows<64, kTreeRowsMax>(a));
+        if (st != PS_OK) return st;
+        for (int32_t r = r0; r < r0 + m; ++r) t0 += n_nodes_host[r];
+    }
+    return PS_OK;
+}
+
+ps_status ps_kv_set_wait_limit(ps_kv* kv, int64_t limit_ns) {
+    if (!kv) return fail(PS_ERR_INVALID, "null argument");
+    if (limit_ns < 0 || limit_ns > kMaxWaitLimitNs) return fail(PS_ERR_INVALID, "limit_ns=%lld outside 0 .. %lld", (long long)limit_ns, (long long)kMaxWaitLimitNs);
+    const_cast<KvPool&>(pool_of(kv)).wait_limit_ns = limit_ns;
+    return PS_OK;
+}
+
+}  // extern "C"

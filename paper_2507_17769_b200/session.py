@@ -32,7 +32,8 @@ def torch_calls():
                 spec = importlib.util.spec_from_file_location(__package__ + "._torch_calls", path)
                 module = importlib.util.module_from_spec(spec)
                 spec.loader.exec_module(module)
-                module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.ps_kv_write, lib.ps_kv_gather, lib.ps_attn_run)))
+                module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.ps_kv_write, lib.ps_kv_gather, lib.ps_attn_run, lib.ps_kv_write_rope,
+                                                                                lib.ps_attn_tree, lib.ps_kv_accept, lib.ps_kv_read)))
                 _torch_calls = module
             except (ImportError, OSError, subprocess.SubprocessError) as e:
                 warnings.warn("the calls with tensors go through addresses: %s" % e, RuntimeWarning)
@@ -53,6 +54,12 @@ class PagedAttention:
     >>> pa.write(k_new, v_new, block_table_dev, prior, q_len)   # cache the new tokens
     >>> pa.plan(prior, q_len, max_pages)                        # host partition
     >>> out, lse = pa.run(q, block_table_dev)                   # attention
+
+    A speculative step, whose new tokens are drafted trees:
+
+    >>> q = pa.write_rope(q, k, v, block_table_dev, prior, n_nodes, cos_sin, positions)   # norms, rotation, append
+    >>> out, lse = pa.run_tree(q, block_table_dev, mask, prior, n_nodes)                  # every node sees its ancestors
+    >>> pa.accept(block_table_dev, prior, n_nodes, index, count)                          # the path that was accepted
     """
 
     def __init__(self, n_q_heads, n_kv_heads, head_dim, num_pages, page_size=16, device="cuda", poison=False, kv_dtype=0):
@@ -77,6 +84,7 @@ class PagedAttention:
         self._ws = None
         self._ws_bytes = 0
         self._ws_ptr = 0
+        self._tree_ws = None
         self._total_q = 0
         self._n_q_heads = int(n_q_heads)
         index = self.pool.device.index
@@ -171,6 +179,53 @@ class PagedAttention:
         B._check(self._calls.attn_run(self._plan, self.kv, q.data_ptr(), block_table_dev.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
                                      self._ws_ptr, self._ws_bytes, self._stream()))
         return out, lse
+
+    # ---- a speculative step ----
+
+    def _steps(self):
+        """The extension, which the calls of a speculative step need: it checks their tensors."""
+        if self._tensor_calls is None:
+            raise RuntimeError("the calls of a speculative step need the extension module for torch tensors, which could be neither loaded nor built")
+        return self._tensor_calls
+
+    def write_rope(self, q, k_new, v_new, block_table_dev, prior, q_len, cos_sin, positions=None, q_weight=None, k_weight=None, eps=1e-6,
+                   interleaved=False, q_out=None):
+        """Append with the norms of queries and keys and the position rotation in the same pass; returns the queries.
+
+        q [T, Hq, d], k_new and v_new [T, Hkv, d]: bf16, may be slices of one projection's output (heads packed, any token stride).
+        cos_sin: float32 [positions, rot_dim], a row's cosines and then its sines, or None: no rotation; rot_dim is a multiple of 16.
+        positions: int32 [T], default the tokens' positions in their sequences.  q_weight, k_weight: bf16 [d], or None: no norm.
+        interleaved: pairs are neighbours instead of halves.  q_out: default a new tensor; q itself where it is packed."""
+        s = self.shape
+        status, q_out = self._steps().write_rope(self.kv, q, k_new, v_new, block_table_dev, B.lengths(prior), B.lengths(q_len), cos_sin, positions, q_weight,
+                                                 k_weight, eps, interleaved, q_out, s.n_q_heads, s.n_kv_heads, s.head_dim, self.pool, self._stream())
+        B._check(status)
+        return q_out
+
+    def run_tree(self, q, block_table_dev, mask, prior, n_nodes, out=None, lse=None, want_lse=True):
+        """Attention for trees of drafted tokens: request r's n_nodes[r] tokens, cached behind its prior[r], see the whole context and
+        the tree tokens of their mask rows.  q: bf16 [T, Hq, d]; mask: int64 [T, words], bit j % 64 of word j / 64 for node j.  Needs no
+        plan.  Returns (out, lse)."""
+        if self._tree_ws is None:
+            self._tree_ws = self.torch.empty(B.ps_attn_tree_workspace(self.shape) + 256, dtype=self.torch.uint8, device=self.device)
+            self._tree_ws_ptr = (self._tree_ws.data_ptr() + 255) // 256 * 256
+        s = self.shape
+        status, out, lse = self._steps().tree(self.kv, q, block_table_dev, mask, B.lengths(prior), B.lengths(n_nodes), out, lse, bool(want_lse), s.n_q_heads,
+                                              s.head_dim, self.pool, self._tree_ws_ptr, self._tree_ws.numel() - 256, self._stream())
+        B._check(status)
+        return out, lse
+
+    def accept(self, block_table_dev, prior, n_nodes, index, count):
+        """Keep an accepted path: position prior[r] + i receives K and V of position prior[r] + index[r, i], i < count[r].
+        index: int32 [n, width], increasing over a row's first count entries; count: int32 [n]; both on the device."""
+        B._check(self._steps().accept(self.kv, block_table_dev, B.lengths(prior), B.lengths(n_nodes), index, count, self.pool, self._stream()))
+
+    def read(self, block_table_dev, begin, length):
+        """Tokens [begin[r], begin[r] + length[r]) of every sequence, packed, as (K, V) bf16 [T, Hkv, d]; an FP8 cache's dequantised."""
+        s = self.shape
+        status, k, v = self._steps().read(self.kv, block_table_dev, B.lengths(begin), B.lengths(length), s.n_kv_heads, s.head_dim, self.pool, self._stream())
+        B._check(status)
+        return k, v
 
     def check(self):
         """Synchronise and raise if the last run saw a device-side error."""
