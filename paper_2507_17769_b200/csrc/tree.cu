@@ -15,12 +15,12 @@
 // follow from the batch's lengths, which travel as kernel parameters: there is no work list to upload and nothing to
 // initialise.
 //
-//   warps 0-3, 4-7  softmax of streams 0 and 1.  The steps (key tile x q tile of 128 rows) of all items alternate between the
-//                   two, so that one stream's exponentials run under the other's products.  With two q tiles each stream keeps one;
-//                   with one q tile the streams take key tiles in turn, with a running maximum, sum and accumulator each, joined
-//                   when the item ends.  Thread t owns row t (TMEM lane t).
+//   warps 0-3, 4-7  softmax of streams 0 and 1; thread t owns row t (TMEM lane t).  A step is 64 keys of 128 rows.  With two q tiles each
+//                   stream has one and takes both halves of every key tile; with one q tile the streams take a half of every key
+//                   tile each, with a running maximum, sum and accumulator of their own, joined when the item ends.
 //   warp 8          K and V tiles: pool blocks gathered by tensor map into one ring, in the order of use K0 K1 V0 K2 V1 ...
-//   warp 9          MMA issue: S = Q K^T (operands in shared memory), O += P V (P as bf16 in the columns that S had)
+//   warp 9          MMA issue: S = Q K^T (operands in shared memory) of two (q tile, key tile) pairs ahead, into two buffers in turn,
+//                   O += P V (P as bf16 in the columns that S had), whichever's operands are there first
 //   warp 10         Q tiles
 //   warp 11         V tiles that hold tree tokens or the sequence's end: rows behind the end become zero, and rows with
 //                   infinities or NaN too, because 0 * inf would reach nodes that do not see them; their weights are added by
@@ -58,8 +58,8 @@ struct Cfg {
     static constexpr int kOffBar = kOffKV + kSlots * kTileBytes;
     // barrier block
     static constexpr int kRaw = kSlots / 2 + 2;              // V tiles on their way through warp 11: more than the ring holds
-    static constexpr int full = 0, empty = full + 8 * kSlots, raw = empty + 8 * kSlots, s_full = raw + 8 * kRaw, p_ready = s_full + 16, o_done = p_ready + 16,
-                         q_full = o_done + 16, q_empty = q_full + 16, ex_full = q_empty + 16, ex_free = ex_full + 8, mma_drained = ex_free + 8,
+    static constexpr int full = 0, empty = full + 8 * kSlots, raw = empty + 8 * kSlots, s_full = raw + 8 * kRaw, p_ready = s_full + 16, pv_done = p_ready + 32,
+                         q_full = pv_done + 32, q_empty = q_full + 16, ex_full = q_empty + 16, ex_free = ex_full + 8, mma_drained = ex_free + 8,
                          n_bars = (mma_drained + 8) / 8;
     static constexpr int tmem_slot = 8 * n_bars, abort_slot = tmem_slot + 4, limit_slot = abort_slot + 4, armed = limit_slot + 4;  // slots, Q tiles, V tiles for warp 11
     static constexpr int flagged = armed + 4 * (kSlots + 2 + kRaw);           // [item % kFlagRing][8]: tree tokens whose V row was taken out
@@ -147,12 +147,14 @@ __device__ __forceinline__ uint32_t mask_word(const uint32_t* row, int w, int no
     const uint32_t x = __ldg(row + w);
     return left < 32 ? x & ((1u << left) - 1u) : x;
 }
-__device__ __forceinline__ uint32_t mask_bits(const uint32_t* row, int at, int nodes) {
+// (w0, w1: the first two words)
+__device__ __forceinline__ uint32_t mask_bits(const uint32_t* row, uint32_t w0, uint32_t w1, int at, int nodes) {
     if (at <= -32) return 0xffffffffu;
-    if (at < 0) return ((1u << -at) - 1u) | mask_word(row, 0, nodes) << -at;
+    if (at < 0) return ((1u << -at) - 1u) | w0 << -at;
+    auto word = [&](int w) { return w == 0 ? w0 : w == 1 ? w1 : mask_word(row, w, nodes); };
     const int w = at >> 5, s = at & 31;
-    const uint32_t lo = mask_word(row, w, nodes);
-    return s == 0 ? lo : __funnelshift_r(lo, mask_word(row, w + 1, nodes), s);
+    const uint32_t lo = word(w);
+    return s == 0 ? lo : __funnelshift_r(lo, word(w + 1), s);
 }
 
 __device__ __forceinline__ bool any_not_finite(const uint4& x) {
@@ -181,8 +183,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         for (int s = 0; s < C::kRaw; ++s) mbar_init(bars + C::raw + 8 * s, 1);
         for (int x = 0; x < 2; ++x) {
             mbar_init(bars + C::s_full + 8 * x, 1);
-            mbar_init(bars + C::p_ready + 8 * x, 4);
-            mbar_init(bars + C::o_done + 8 * x, 1);
+            mbar_init(bars + C::p_ready + 16 * x, 4);
+            mbar_init(bars + C::p_ready + 16 * x + 8, 4);
+            mbar_init(bars + C::pv_done + 16 * x, 1);
+            mbar_init(bars + C::pv_done + 16 * x + 8, 1);
             mbar_init(bars + C::q_full + 8 * x, 1);
             mbar_init(bars + C::q_empty + 8 * x, 1);
         }
@@ -219,50 +223,53 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
         const int x = warp >> 2, t = threadIdx.x & 127;
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t s_addr = tmem + lane_addr + x * 128;
         constexpr float kScaleLog2 = scale_log2(D);
-        uint32_t g = 0, steps_x = 0, items_x = 0, n_item = 0, n_ex = 0;  // steps of all items; of this stream: steps and items with any; items; exchanges
+        uint32_t g = 0, steps = 0, n_item = 0, n_ex = 0;  // QK^Ts of the items before; steps of this stream; items; exchanges
         bool ok = true, must_wait_free = false;
+        // PV of a step; the one before it was complete when the scores after it were, so of two barriers in turn neither is a phase behind or ahead
+        auto pv_wait = [&](uint32_t step) { return wait_all(bars + C::pv_done + 16 * x + 8 * (step & 1), (step >> 1) & 1, s_abort); };
         while (ok && iter.next(it)) {
-            const int n_x = it.n_x(p.G), n_tiles = it.tile1 - it.tile0, n_steps = n_tiles * n_x;
-            const int first = (int)((x - g) & 1);                    // this stream's first step of the item
-            const int q_tile = n_x == 2 ? first : 0;
+            const int n_x = it.n_x(p.G), n_tiles = it.tile1 - it.tile0;
+            const int q_tile = n_x == 2 ? (int)((x - g) & 1) : 0;
             const int row_tok = q_tile * tile_tok + (t >> g_shift);  // token of this row within the item
             const bool valid = row_tok < it.n_tok;
-            const bool warp_valid = q_tile * tile_tok + (((t & ~31)) >> g_shift) < it.n_tok;  // any row of this warp
+            const bool warp_valid = q_tile * tile_tok + ((t & ~31) >> g_shift) < it.n_tok;  // any row of this warp
             const int64_t token = it.q_tok + row_tok;
             const uint32_t* const mask_row = p.mask + token * 2 * p.mask_words;
+            // (the first 64 nodes' are wanted soon enough to ask for them now)
+            const uint32_t mask0 = valid ? mask_word(mask_row, 0, it.nodes) : 0u, mask1 = valid ? mask_word(mask_row, 1, it.nodes) : 0u;
             float m = -INFINITY, l = 0.f, lu = 0.f;  // running maximum (log2 units), sums of the rounded and of the exact weights
-            int mine = 0;
-            for (int s = first; s < n_steps; s += 2, ++mine) {
-                ok = wait_all(bars + C::s_full + 8 * x, steps_x & 1, s_abort);
-                if (!ok) break;
-                ++steps_x;
-                tc_fence_after();
+            for (int k = 0; k < n_tiles * n_x; ++k) {
+                const int tile = n_x == 2 ? k >> 1 : k, half = n_x == 2 ? k & 1 : x;
+                const uint32_t u = n_x == 2 ? g + 2 * tile + q_tile : g + k, buf = u & 1;
+                if (n_x == 1 || half == 0) {
+                    ok = wait_all(bars + C::s_full + 8 * buf, (u >> 1) & 1, s_abort);
+                    if (!ok) break;
+                    tc_fence_after();
+                }
                 if (warp_valid) {
-                    const int key0 = (it.tile0 + (n_x == 2 ? s >> 1 : s)) * kTileKeys;
-                    const bool masked = key0 + kTileKeys > it.prior;
-                    uint32_t sv[4][32];
+                    const uint32_t s_addr = tmem + lane_addr + buf * 128 + half * 64;
+                    const int key0 = (it.tile0 + tile) * kTileKeys + half * 64;
+                    const bool masked = key0 + 64 > it.prior;
+                    uint32_t sv[2][32];
                     tmem_ld32(s_addr, sv[0]);
                     tmem_ld32(s_addr + 32, sv[1]);
-                    tmem_ld32(s_addr + 64, sv[2]);
-                    tmem_ld32(s_addr + 96, sv[3]);
-                    uint32_t vis[4];
+                    uint32_t vis[2];
                     if (masked) {
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) vis[q] = valid ? mask_bits(mask_row, key0 + 32 * q - it.prior, it.nodes) : 0u;
+                        for (int q = 0; q < 2; ++q) vis[q] = valid ? mask_bits(mask_row, mask0, mask1, key0 + 32 * q - it.prior, it.nodes) : 0u;
                     }
                     tmem_wait_ld();
                     if (masked) {
 #pragma unroll
-                        for (int q = 0; q < 4; ++q)
+                        for (int q = 0; q < 2; ++q)
 #pragma unroll
                             for (int c = 0; c < 32; ++c)
                                 if (!(vis[q] >> c & 1u)) sv[q][c] = 0xff800000u;
                     }
                     float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
+                    for (int q = 0; q < 2; ++q)
 #pragma unroll
                         for (int c = 0; c < 32; c += 8) {
                             mx0 = max3(mx0, __uint_as_float(sv[q][c]), __uint_as_float(sv[q][c + 1]));
@@ -273,8 +280,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                     const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * kScaleLog2;
                     const float m_new = mx > m + kRescaleThreshold ? mx : m;  // also the first finite maximum
                     const float alpha = m_new == m ? 1.f : fast_exp2(m - m_new);
-                    // (the commit that raised s_full came after this stream's last PV)
-                    if (mine > 0 && __any_sync(0xffffffffu, m_new != m)) {
+                    if (k > 0 && __any_sync(0xffffffffu, m_new != m)) {
+                        // the accumulator as of the step before (what came before that was complete when these scores were)
+                        ok = pv_wait(steps - 1);
+                        if (!ok) break;
+                        tc_fence_after();
                         const uint32_t o_addr = tmem + lane_addr + kColO + x * D;
 #pragma unroll 1
                         for (int c0 = 0; c0 < D; c0 += 32) {
@@ -295,28 +305,23 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                     // (masked scores are -inf, and their weights exp2(-inf) = 0)
                     uint64_t ls0 = 0ull, ls1 = 0ull;
                     float l0 = 0.f, l1 = 0.f;
+                    uint32_t packed[32];
 #pragma unroll
-                    for (int hhalf = 0; hhalf < 2; ++hhalf) {
-                        uint32_t packed[32];
+                    for (int q = 0; q < 2; ++q)
 #pragma unroll
-                        for (int qq = 0; qq < 2; ++qq) {
-                            const int q = hhalf * 2 + qq;
-#pragma unroll
-                            for (int c = 0; c < 32; c += 2) {
-                                float e0, e1;
-                                unpack2(fma2(pack2(__uint_as_float(sv[q][c]), __uint_as_float(sv[q][c + 1])), sc2, nm2), e0, e1);
-                                e0 = fast_exp2(e0), e1 = fast_exp2(e1);
-                                if (c & 2) ls1 = add2(ls1, pack2(e0, e1));
-                                else ls0 = add2(ls0, pack2(e0, e1));
-                                packed[qq * 16 + (c >> 1)] = pack_bf16(e0, e1);
-                                if (masked) {
-                                    // (rows of few keys: the sum of the weights that PV multiplies keeps the output an exact mix of V rows)
-                                    l0 += bf16_lo(packed[qq * 16 + (c >> 1)]);
-                                    l1 += bf16_hi(packed[qq * 16 + (c >> 1)]);
-                                }
-                            }
+                        for (int c = 0; c < 32; c += 2) {
+                            float e0, e1;
+                            unpack2(fma2(pack2(__uint_as_float(sv[q][c]), __uint_as_float(sv[q][c + 1])), sc2, nm2), e0, e1);
+                            e0 = fast_exp2(e0), e1 = fast_exp2(e1);
+                            if (c & 2) ls1 = add2(ls1, pack2(e0, e1));
+                            else ls0 = add2(ls0, pack2(e0, e1));
+                            packed[q * 16 + (c >> 1)] = pack_bf16(e0, e1);
                         }
-                        tmem_st32(s_addr + hhalf * 32, packed);
+                    tmem_st32(s_addr, packed);
+                    if (masked) {
+                        // (rows of few keys: the sum of the weights that PV multiplies keeps the output an exact mix of V rows)
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) l0 += bf16_lo(packed[c]), l1 += bf16_hi(packed[c]);
                     }
                     float a0, a1, a2, a3;
                     unpack2(ls0, a0, a1);
@@ -326,6 +331,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                     l += masked ? l0 + l1 : sum;
                     tmem_wait_st();
                 }
+                ++steps;
                 if (must_wait_free) {
                     // the other stream's warps have read this stream's last accumulator, which the product to come overwrites
                     ok = wait_all(bars + C::ex_free, (n_ex & 1) ^ 1, s_abort);
@@ -334,27 +340,18 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bars + C::p_ready + 8 * x);
+                if (lane == 0) mbar_arrive(bars + C::p_ready + 16 * buf + 8 * half);
             }
             if (!ok) break;
             // ---- the item's end ----
-            if (mine > 0) {
-                ok = wait_all(bars + C::o_done + 8 * x, items_x & 1, s_abort);
-                if (!ok) break;
-                ++items_x;
-                tc_fence_after();
-            }
+            ok = pv_wait(steps - 1);
+            if (!ok) break;
+            tc_fence_after();
             float w0 = 1.f, w1 = 0.f;  // weights of the accumulators (streams 0 and 1 where both have a part of the row)
             int col0 = 0, col1 = D;
             uint32_t o0 = tmem + lane_addr + kColO + x * D, o1 = o0;
-            bool both = false;
             if (n_x == 1) {
                 // rows of one q tile: join the streams; each writes half of the columns
-                if (must_wait_free) {
-                    ok = wait_all(bars + C::ex_free, (n_ex & 1) ^ 1, s_abort);
-                    if (!ok) break;
-                    must_wait_free = false;
-                }
                 exchange[x * kRows + t] = make_float2(m, lu);
                 rounding[x * kRows + t] = __float2half_rn(lu > 0.f ? (l - lu) / lu : 0.f);
                 tc_fence_before();
@@ -367,18 +364,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                 const float ra = 1.f + __half2float(rounding[t]), rb = 1.f + __half2float(rounding[kRows + t]);
                 ++n_ex;
                 must_wait_free = true;
-                const bool has0 = n_steps > 1 || (g & 1) == 0, has1 = n_steps > 1 || (g & 1) == 1;
-                both = has0 && has1;
-                m = fmaxf(has0 ? a.x : -INFINITY, has1 ? b.x : -INFINITY);
+                m = fmaxf(a.x, b.x);
                 const float m_sub = m == -INFINITY ? 0.f : m;
-                w0 = has0 ? fast_exp2(a.x - m_sub) : 0.f;
-                w1 = has1 ? fast_exp2(b.x - m_sub) : 0.f;
-                const float lu0 = has0 ? a.y * w0 : 0.f, lu1 = has1 ? b.y * w1 : 0.f;
+                w0 = fast_exp2(a.x - m_sub);
+                w1 = fast_exp2(b.x - m_sub);
+                const float lu0 = a.y * w0, lu1 = b.y * w1;
                 lu = lu0 + lu1;
                 l = lu0 * ra + lu1 * rb;
                 o0 = tmem + lane_addr + kColO;
                 o1 = o0 + D;
-                if (!has0) o0 = o1, w0 = w1;
                 col0 = x * (D / 2);
                 col1 = col0 + D / 2;
             }
@@ -396,7 +390,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                 for (int c0 = col0; c0 < col1; c0 += 32) {
                     uint32_t v[32];
                     tmem_ld32(o0 + c0, v);
-                    if (both) {
+                    if (n_x == 1) {
                         uint32_t u[32];
                         tmem_ld32(o1 + c0, u);
                         tmem_wait_ld();
@@ -404,10 +398,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                         for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(fmaf(__uint_as_float(v[c]), w0, __uint_as_float(u[c]) * w1));
                     } else {
                         tmem_wait_ld();
-                        if (n_x == 1) {
-#pragma unroll
-                            for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(__uint_as_float(v[c]) * w0);
-                        }
                     }
                     if (flags && valid) {
                         // tree tokens whose V row was taken out of the products: their weight times that row
@@ -457,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bars + C::ex_free);
             }
-            g += n_steps;
+            g += n_tiles * n_x;
             ++n_item;
         }
     } else {
@@ -540,7 +530,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
             }
         } else if (warp == kMmaWarp) {
             // ================================================================
-            // MMA issue: QK^T of step i + 2 behind PV of step i, across items
+            // MMA issue.  QK^T number u (of all items: key tile by key tile, q tile by q tile) goes to buffer u & 1 once both PVs of number
+            // u - 2 have been issued; a PV takes the 64 weights of one step.
             // ================================================================
             constexpr uint32_t kIdescQK = instr_desc(kRows, kTileKeys, false), kIdescPV = instr_desc(kRows, D, true);
             const uint64_t desc_kmajor = smem_desc(0, 16, 1024), desc_v = smem_desc(0, C::kHalfBytes, 1024);
@@ -548,41 +539,67 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
             Piece iv;
             bool ok = true;
             uint32_t k_tile = 0, v_tile = 0;         // tiles that QK^T and PV have finished
-            uint32_t gk = 0, gv = 0;                 // steps that they have issued
+            uint32_t gk = 0, gv = 0;                 // QK^Ts issued; of them, those whose PVs have been
             uint32_t q_tiles = 0;                    // q tiles of the items before QK^T's
-            int sk = 0, nk = 0, xk = 1, sv = 0, nv = 0, xv = 1;  // step within the item, its steps, its q tiles
+            int sk = 0, nk = 0, xk = 1;              // QK^T within the item, its number of them, its q tiles
+            int sv = 0, nv = 0, xv = 1, hv = 0;      // the same of PV, and the half
+            uint32_t pv_steps = 0;                   // bit x: parity of stream x's steps
             bool have_k = true;
-            while (ok) {
-                if (have_k && gk - gv < 2) {
-                    if (sk == nk) {
-                        if (nk > 0) q_tiles += xk;
-                        have_k = iter.next(it);
-                        if (!have_k) continue;
-                        xk = it.n_x(p.G);
-                        nk = (it.tile1 - it.tile0) * xk;
-                        sk = 0;
+            // which of two phases is complete first, polled for at most about the wait limit: 1, 2, or 0
+            auto either = [&](uint32_t bar1, uint32_t par1, uint32_t bar2, uint32_t par2) {
+                uint32_t t0 = 0;
+                for (uint32_t i = 1;; ++i) {
+                    if (__all_sync(0xffffffffu, mbar_test_wait(bar1, par1))) return 1;
+                    if (__all_sync(0xffffffffu, mbar_test_wait(bar2, par2))) return 2;
+                    const uint32_t limit_ns = (uint32_t)s_abort[1];
+                    if ((i & (kWaitPollsPerClockRead - 1)) == 0 || limit_ns == 0) {
+                        const uint32_t now = global_timer_lo() | 1u;
+                        if (t0 == 0) t0 = now;
+                        if (__any_sync(0xffffffffu, *s_abort || limit_ns == 0 || now - t0 > limit_ns)) break;
                     }
-                    const int qt = xk == 2 ? sk & 1 : 0;
-                    const bool tile_ends = xk == 1 || qt == 1;
-                    const uint32_t e = k_tile == 0 ? 0 : 2 * k_tile - 1, s = e % C::kSlots, qn = q_tiles + qt, qs = qn & 1;
+                }
+                *s_abort = 1;
+                return 0;
+            };
+            while (ok) {
+                if (have_k && sk == nk) {
+                    if (nk > 0) q_tiles += xk;
+                    have_k = iter.next(it);
+                    xk = it.n_x(p.G);
+                    nk = have_k ? (it.tile1 - it.tile0) * xk : 0;
+                    sk = 0;
+                }
+                if (gv == gk && !have_k) break;
+                const int qt = xk == 2 ? sk & 1 : 0;
+                const uint32_t ek = k_tile == 0 ? 0 : 2 * k_tile - 1, ks = ek % C::kSlots;
+                bool do_qk = have_k && gk - gv < 2;
+                if (do_qk && qt == 0) {
+                    if (gv == gk) {
+                        ok = wait_all(bars + C::full + 8 * ks, (ek / C::kSlots) & 1, s_abort);
+                    } else {
+                        const int which = either(bars + C::full + 8 * ks, (ek / C::kSlots) & 1, bars + C::p_ready + 16 * (gv & 1) + 8 * hv, (gv >> 1) & 1);
+                        ok = which != 0;
+                        do_qk = which == 1;
+                    }
+                    if (!ok) break;
+                }
+                if (do_qk) {
+                    const uint32_t qn = q_tiles + qt, qs = qn & 1;
                     if (sk < xk) {
                         ok = wait_all(bars + C::q_full + 8 * qs, (qn >> 1) & 1, s_abort);
                         if (!ok) break;
                     }
-                    if (qt == 0) {
-                        ok = wait_all(bars + C::full + 8 * s, (e / C::kSlots) & 1, s_abort);
-                        if (!ok) break;
-                    }
+                    const bool tile_ends = xk == 1 || qt == 1;
                     tc_fence_after();
                     if (elect_one()) {
-                        const uint64_t qd = desc_kmajor + ((sbase + C::kOffQ + qs * C::kTileBytes) >> 4), kd = desc_kmajor + ((sbase + C::kOffKV + s * C::kTileBytes) >> 4);
+                        const uint64_t qd = desc_kmajor + ((sbase + C::kOffQ + qs * C::kTileBytes) >> 4), kd = desc_kmajor + ((sbase + C::kOffKV + ks * C::kTileBytes) >> 4);
 #pragma unroll
                         for (int kk = 0; kk < D / 16; ++kk) {
                             const uint32_t off = ((kk >> 2) * C::kHalfBytes + (kk & 3) * 32) >> 4;
                             tc_mma_ss(tmem + (gk & 1) * 128, qd + off, kd + off, kIdescQK, kk > 0);
                         }
                         tc_commit(bars + C::s_full + 8 * (gk & 1));
-                        if (tile_ends) tc_commit(bars + C::empty + 8 * s);
+                        if (tile_ends) tc_commit(bars + C::empty + 8 * ks);
                         if (sk + xk >= nk) tc_commit(bars + C::q_empty + 8 * qs);
                     }
                     __syncwarp();
@@ -591,34 +608,37 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                     ++gk;
                     continue;
                 }
-                if (gv == gk) break;
                 if (sv == nv) {
                     iter_v.next(iv);
                     xv = iv.n_x(p.G);
                     nv = (iv.tile1 - iv.tile0) * xv;
                     sv = 0;
                 }
-                const bool tile_begins = xv == 1 || (sv & 1) == 0, tile_ends = xv == 1 || (sv & 1) == 1;
-                const uint32_t e = 2 * v_tile + 2, s = e % C::kSlots, x = gv & 1;
-                if (tile_begins) {
-                    ok = wait_all(bars + C::full + 8 * s, (e / C::kSlots) & 1, s_abort);
+                const uint32_t ev = 2 * v_tile + 2, vs = ev % C::kSlots, buf = gv & 1, x = xv == 2 ? buf : hv;
+                if (hv == 0 && (xv == 1 || (sv & 1) == 0)) {
+                    ok = wait_all(bars + C::full + 8 * vs, (ev / C::kSlots) & 1, s_abort);
                     if (!ok) break;
                 }
-                ok = wait_all(bars + C::p_ready + 8 * x, (gv >> 1) & 1, s_abort);
+                ok = wait_all(bars + C::p_ready + 16 * buf + 8 * hv, (gv >> 1) & 1, s_abort);
                 if (!ok) break;
+                const bool tile_ends = hv == 1 && (xv == 1 || (sv & 1) == 1), first = xv == 2 ? sv < 2 && hv == 0 : sv == 0;
                 tc_fence_after();
                 if (elect_one()) {
-                    const uint64_t vd = desc_v + ((sbase + C::kOffKV + s * C::kTileBytes) >> 4);
+                    const uint64_t vd = desc_v + ((sbase + C::kOffKV + vs * C::kTileBytes) >> 4) + hv * 4 * (2048 >> 4);
 #pragma unroll
-                    for (int kk = 0; kk < kTileKeys / 16; ++kk)
-                        tc_mma_ts(tmem + kColO + x * D, tmem + x * 128 + kk * 8, vd + kk * (2048 >> 4), kIdescPV, (sv >= 2 || kk > 0) ? 1u : 0u);
-                    if (tile_ends) tc_commit(bars + C::empty + 8 * s);
-                    if (sv + 2 >= nv) tc_commit(bars + C::o_done + 8 * x);
+                    for (int kk = 0; kk < 4; ++kk)
+                        tc_mma_ts(tmem + kColO + x * D, tmem + buf * 128 + hv * 64 + kk * 8, vd + kk * (2048 >> 4), kIdescPV, (!first || kk > 0) ? 1u : 0u);
+                    tc_commit(bars + C::pv_done + 16 * x + 8 * (pv_steps >> x & 1));
+                    if (tile_ends) tc_commit(bars + C::empty + 8 * vs);
                 }
                 __syncwarp();
+                pv_steps ^= 1u << x;
                 if (tile_ends) ++v_tile;
-                ++sv;
-                ++gv;
+                hv ^= 1;
+                if (hv == 0) {
+                    ++sv;
+                    ++gv;
+                }
             }
         } else if (warp == kQWarp) {
             // ================================================================

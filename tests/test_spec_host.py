@@ -147,7 +147,7 @@ def test_refusals_of_the_library():
     refused(inv, tree, [0, 0], [65 - 1, 0])
     refused(inv, tree, [-1, 0], [3, 1])
     refused(uns, tree, [0, 0], [3, 1], 5)
-    refused(uns, tree, [0, 0], [3, 1], 0)
+    refused(inv, tree, [0, 0], [3, 1], 0)  # (an empty tensor has no address)
     long = torch.zeros((1, 20), dtype=I32, device="cuda")
     refused(inv, pa.run_tree, torch.zeros((65, HQ, D), dtype=BF, device="cuda"), long, torch.zeros((65, 1), dtype=I64, device="cuda"), [0], [65])
     ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
