@@ -17,12 +17,12 @@
 //
 //   warps 0-3, 4-7  softmax of streams 0 and 1; thread t owns row t (TMEM lane t).  A step is 64 keys of 128 rows.  With two q tiles each
 //                   stream has one and takes both halves of every key tile; with one q tile the streams take a half of every key
-//                   tile each, with a running maximum, sum and accumulator of their own, joined when the item ends.
+//                   tile each, with a running maximum, sum and accumulator of their own, joined when the item ends.  Results go out
+//                   through the Q tile's place, so that global stores cover whole sectors of a row.
 //   warp 8          K and V tiles: pool blocks gathered by tensor map into one ring, in the order of use K0 K1 V0 K2 V1 ...
-//   warp 9          MMA issue: S = Q K^T (operands in shared memory) of two (q tile, key tile) pairs ahead, into two buffers in turn,
+//   warps 9, 10     MMA issue of streams 0 and 1: S = Q K^T (operands in shared memory) two steps ahead, into two buffers in turn,
 //                   O += P V (P as bf16 in the columns that S had), whichever's operands are there first
-//   warp 10         Q tiles
-//   warp 11         V tiles that hold tree tokens or the sequence's end: rows behind the end become zero, and rows with
+//   warp 11         Q tiles; and V tiles that hold tree tokens or the sequence's end: rows behind the end become zero, and rows with
 //                   infinities or NaN too, because 0 * inf would reach nodes that do not see them; their weights are added by
 //                   the rows that do when the item ends.
 //
@@ -35,9 +35,8 @@ namespace ps {
 
 namespace {
 
-constexpr int kThreads = 384;
-constexpr int kRegsSoftmax = 192, kRegsOther = 120;  // 384 x 168 at launch = 256 x 192 + 128 x 120
-constexpr int kLoadWarp = 8, kMmaWarp = 9, kQWarp = 10;  // (11: rows of V)
+constexpr int kThreads = 384;  // three warps a scheduler: 168 registers each
+constexpr int kLoadWarp = 8, kMmaWarp = 9;  // (MMA: 9 and 10; Q and rows of V: 11)
 constexpr int kTileKeys = 128, kRows = 128;
 constexpr int kGroupRows = 2 * kRows;      // rows of an item
 constexpr int kMaxNodes = 256;
@@ -58,9 +57,10 @@ struct Cfg {
     static constexpr int kOffBar = kOffKV + kSlots * kTileBytes;
     // barrier block
     static constexpr int kRaw = kSlots / 2 + 2;              // V tiles on their way through warp 11: more than the ring holds
-    static constexpr int full = 0, empty = full + 8 * kSlots, raw = empty + 8 * kSlots, s_full = raw + 8 * kRaw, p_ready = s_full + 16, pv_done = p_ready + 32,
-                         q_full = pv_done + 32, q_empty = q_full + 16, ex_full = q_empty + 16, ex_free = ex_full + 8, mma_drained = ex_free + 8,
-                         n_bars = (mma_drained + 8) / 8;
+    static constexpr int full = 0, empty = full + 8 * kSlots, raw = empty + 8 * kSlots;
+    // [stream][its step & 1]: scores there, weights there, product with V done
+    static constexpr int s_full = raw + 8 * kRaw, p_ready = s_full + 32, pv_done = p_ready + 32;
+    static constexpr int q_full = pv_done + 32, q_empty = q_full + 16, ex_full = q_empty + 16, ex_free = ex_full + 8, mma_drained = ex_free + 8, n_bars = (mma_drained + 8) / 8;
     static constexpr int tmem_slot = 8 * n_bars, abort_slot = tmem_slot + 4, limit_slot = abort_slot + 4, armed = limit_slot + 4;  // slots, Q tiles, V tiles for warp 11
     static constexpr int flagged = armed + 4 * (kSlots + 2 + kRaw);           // [item % kFlagRing][8]: tree tokens whose V row was taken out
     static constexpr int exchange = (flagged + kFlagRing * 32 + 7) / 8 * 8;   // [stream][row] (maximum, sum of the weights)
@@ -89,7 +89,7 @@ struct TreeParams {
     int* flag;
     int64_t num_pages;
     uint32_t wait_limit_ns;
-    int32_t max_pages, mask_words, n, Hq, Hkv, G, units;
+    int32_t max_pages, mask_words, n, Hq, Hkv, G, units, share, longer;  // a share's units; the first `longer` shares have one more
 };
 
 // pieces of items in a CTA's share of the line
@@ -101,7 +101,7 @@ struct Piece {
     // first tile with tree tokens or the sequence's end in it
     __device__ __forceinline__ int tree_tile() const { return prior / kTileKeys; }
 };
-__device__ __forceinline__ int share_begin(int units, int c, int n_cta) { return (int)((int64_t)units * c / n_cta); }
+__device__ __forceinline__ int share_begin(const TreeParams& p, int c) { return c * p.share + min(c, p.longer); }
 
 template <class Rows>
 struct PieceIter {
@@ -129,8 +129,8 @@ struct PieceIter {
             x.tile0 = max(0, w0 - kItemUnits);
             x.tile1 = max(0, w1 - kItemUnits);
             if (x.tile1 <= x.tile0) continue;
-            const int group_tok = kGroupRows / G, groups = (x.nodes + group_tok - 1) / group_tok;
-            x.head = item / groups;
+            const int shift = 31 - __clz(kGroupRows / G), group_tok = 1 << shift, groups = (x.nodes + group_tok - 1) >> shift;  // (G is a power of two)
+            x.head = groups == 1 ? item : item / groups;
             x.tok0 = (item - x.head * groups) * group_tok;
             x.n_tok = min(group_tok, x.nodes - x.tok0);
             x.q_tok += x.tok0;
@@ -140,21 +140,42 @@ struct PieceIter {
     }
 };
 
-// 32 bits of a row's mask from node `at` on; nodes before the tree are context and visible, behind its end there is nothing
-__device__ __forceinline__ uint32_t mask_word(const uint32_t* row, int w, int nodes) {
+// Word w of a row's mask without the bits behind the last node
+__device__ __forceinline__ uint32_t up_to(uint32_t x, int w, int nodes) {
     const int left = nodes - 32 * w;
-    if (left <= 0) return 0u;
-    const uint32_t x = __ldg(row + w);
-    return left < 32 ? x & ((1u << left) - 1u) : x;
+    return left >= 32 ? x : left <= 0 ? 0u : x & ((1u << left) - 1u);
 }
-// (w0, w1: the first two words)
+__device__ __forceinline__ uint32_t mask_word(const uint32_t* row, int w, int nodes) { return 32 * w < nodes ? up_to(__ldg(row + w), w, nodes) : 0u; }
+// 32 bits of a row's mask from node `at` on; nodes before the tree are context and visible, behind its end there is nothing (w0, w1: the first two
+// words as they stand)
 __device__ __forceinline__ uint32_t mask_bits(const uint32_t* row, uint32_t w0, uint32_t w1, int at, int nodes) {
     if (at <= -32) return 0xffffffffu;
-    if (at < 0) return ((1u << -at) - 1u) | w0 << -at;
-    auto word = [&](int w) { return w == 0 ? w0 : w == 1 ? w1 : mask_word(row, w, nodes); };
+    if (at < 0) return ((1u << -at) - 1u) | up_to(w0, 0, nodes) << -at;
+    auto word = [&](int w) { return w < 2 ? up_to(w == 0 ? w0 : w1, w, nodes) : mask_word(row, w, nodes); };
     const int w = at >> 5, s = at & 31;
     const uint32_t lo = word(w);
     return s == 0 ? lo : __funnelshift_r(lo, word(w + 1), s);
+}
+
+// A warp's 32 rows of BYTES each, a row a lane, through its stage, so that stores cover BYTES of a row: dst(row) is where a row goes, or null.
+// (Units of 16 bytes change places row by row against bank conflicts.)
+template <int BYTES, class F>
+__device__ __forceinline__ void store_rows(char* stage, int lane, const uint32_t* v, const F& dst) {
+    constexpr int U = BYTES / 16;  // units of a row
+    auto place = [&](int row, int u) { return stage + row * BYTES + ((u ^ (U == 8 ? row & 7 : row >> 1 & 3)) << 4); };
+#pragma unroll
+    for (int u = 0; u < U; ++u) *reinterpret_cast<uint4*>(place(lane, u)) = make_uint4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
+    __syncwarp();
+    // (all loads first: the compiler cannot tell that the stores go elsewhere)
+    uint4 x[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) x[k] = *reinterpret_cast<const uint4*>(place(k * (32 / U) + lane / U, lane % U));
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        char* const to = dst(k * (32 / U) + lane / U);
+        if (to) *reinterpret_cast<uint4*>(to + 16 * (lane % U)) = x[k];
+    }
+    __syncwarp();
 }
 
 __device__ __forceinline__ bool any_not_finite(const uint4& x) {
@@ -178,21 +199,21 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::kSlots; ++s) {
             mbar_init(bars + C::full + 8 * s, 1);
-            mbar_init(bars + C::empty + 8 * s, 1);
+            mbar_init(bars + C::empty + 8 * s, 2);
         }
         for (int s = 0; s < C::kRaw; ++s) mbar_init(bars + C::raw + 8 * s, 1);
+        for (int k = 0; k < 4; ++k) {
+            mbar_init(bars + C::s_full + 8 * k, 1);
+            mbar_init(bars + C::p_ready + 8 * k, 4);
+            mbar_init(bars + C::pv_done + 8 * k, 1);
+        }
         for (int x = 0; x < 2; ++x) {
-            mbar_init(bars + C::s_full + 8 * x, 1);
-            mbar_init(bars + C::p_ready + 16 * x, 4);
-            mbar_init(bars + C::p_ready + 16 * x + 8, 4);
-            mbar_init(bars + C::pv_done + 16 * x, 1);
-            mbar_init(bars + C::pv_done + 16 * x + 8, 1);
             mbar_init(bars + C::q_full + 8 * x, 1);
-            mbar_init(bars + C::q_empty + 8 * x, 1);
+            mbar_init(bars + C::q_empty + 8 * x, 8);
         }
         mbar_init(bars + C::ex_full, 8);
         mbar_init(bars + C::ex_free, 8);
-        mbar_init(bars + C::mma_drained, 1);
+        mbar_init(bars + C::mma_drained, 2);
         mbar_fence_init();
         s_abort[0] = 0;
         s_abort[1] = (int)p.wait_limit_ns;
@@ -210,9 +231,25 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + C::kOffBar + C::tmem_slot);
     auto wait_all = [](uint32_t bar, uint32_t parity, volatile int* abort_flag) { return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag)); };
 
+    // which of two phases is complete first, polled for at most about the wait limit: 1, 2, or 0
+    auto either = [&](uint32_t bar1, uint32_t par1, uint32_t bar2, uint32_t par2) {
+        uint32_t t0 = 0;
+        for (uint32_t i = 1;; ++i) {
+            if (__all_sync(0xffffffffu, mbar_test_wait(bar1, par1))) return 1;
+            if (__all_sync(0xffffffffu, mbar_test_wait(bar2, par2))) return 2;
+            const uint32_t limit_ns = (uint32_t)s_abort[1];
+            if ((i & (kWaitPollsPerClockRead - 1)) == 0 || limit_ns == 0) {
+                const uint32_t now = global_timer_lo() | 1u;
+                if (t0 == 0) t0 = now;
+                if (__any_sync(0xffffffffu, *s_abort || limit_ns == 0 || now - t0 > limit_ns)) break;
+            }
+        }
+        *s_abort = 1;
+        return 0;
+    };
+
     constexpr uint32_t kColO = 256;
-    const int share0 = share_begin(p.units, blockIdx.x, gridDim.x), share1 = share_begin(p.units, blockIdx.x + 1, gridDim.x);
-    PieceIter<Rows> iter(rows, p.n, p.G, share0, share1);
+    PieceIter<Rows> iter(rows, p.n, p.G, share_begin(p, blockIdx.x), share_begin(p, blockIdx.x + 1));
     Piece it;
     const int tile_tok = kRows / p.G, g_shift = 31 - __clz(p.G);
 
@@ -220,35 +257,33 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         // ====================================================================
         // softmax
         // ====================================================================
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
         const int x = warp >> 2, t = threadIdx.x & 127;
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
         constexpr float kScaleLog2 = scale_log2(D);
-        uint32_t g = 0, steps = 0, n_item = 0, n_ex = 0;  // QK^Ts of the items before; steps of this stream; items; exchanges
+        uint32_t steps = 0, q_tiles = 0, n_item = 0, n_ex = 0;  // of this stream; of the items before; items; exchanges
         bool ok = true, must_wait_free = false;
-        // PV of a step; the one before it was complete when the scores after it were, so of two barriers in turn neither is a phase behind or ahead
-        auto pv_wait = [&](uint32_t step) { return wait_all(bars + C::pv_done + 16 * x + 8 * (step & 1), (step >> 1) & 1, s_abort); };
-        while (ok && iter.next(it)) {
+        Piece ahead;
+        bool more = iter.next(ahead);
+        while (ok && more) {
+            it = ahead;
             const int n_x = it.n_x(p.G), n_tiles = it.tile1 - it.tile0;
-            const int q_tile = n_x == 2 ? (int)((x - g) & 1) : 0;
+            const int q_tile = n_x == 2 ? x : 0;
             const int row_tok = q_tile * tile_tok + (t >> g_shift);  // token of this row within the item
             const bool valid = row_tok < it.n_tok;
             const bool warp_valid = q_tile * tile_tok + ((t & ~31) >> g_shift) < it.n_tok;  // any row of this warp
             const int64_t token = it.q_tok + row_tok;
             const uint32_t* const mask_row = p.mask + token * 2 * p.mask_words;
             // (the first 64 nodes' are wanted soon enough to ask for them now)
-            const uint32_t mask0 = valid ? mask_word(mask_row, 0, it.nodes) : 0u, mask1 = valid ? mask_word(mask_row, 1, it.nodes) : 0u;
+            const uint32_t mask0 = valid ? __ldg(mask_row) : 0u, mask1 = valid ? __ldg(mask_row + 1) : 0u;
             float m = -INFINITY, l = 0.f, lu = 0.f;  // running maximum (log2 units), sums of the rounded and of the exact weights
             for (int k = 0; k < n_tiles * n_x; ++k) {
                 const int tile = n_x == 2 ? k >> 1 : k, half = n_x == 2 ? k & 1 : x;
-                const uint32_t u = n_x == 2 ? g + 2 * tile + q_tile : g + k, buf = u & 1;
-                if (n_x == 1 || half == 0) {
-                    ok = wait_all(bars + C::s_full + 8 * buf, (u >> 1) & 1, s_abort);
-                    if (!ok) break;
-                    tc_fence_after();
-                }
+                const uint32_t buf = steps & 1;
+                ok = wait_all(bars + C::s_full + 16 * x + 8 * buf, (steps >> 1) & 1, s_abort);
+                if (!ok) break;
+                tc_fence_after();
                 if (warp_valid) {
-                    const uint32_t s_addr = tmem + lane_addr + buf * 128 + half * 64;
+                    const uint32_t s_addr = tmem + lane_addr + x * 128 + buf * 64;
                     const int key0 = (it.tile0 + tile) * kTileKeys + half * 64;
                     const bool masked = key0 + 64 > it.prior;
                     uint32_t sv[2][32];
@@ -260,6 +295,43 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                         for (int q = 0; q < 2; ++q) vis[q] = valid ? mask_bits(mask_row, mask0, mask1, key0 + 32 * q - it.prior, it.nodes) : 0u;
                     }
                     tmem_wait_ld();
+                    const uint64_t sc2 = pack2(kScaleLog2, kScaleLog2);
+                    bool done = false;
+                    if (!masked && k > 0) {
+                        // Nearly every step leaves the running maximum as it is: weights and maximum at once, and again where one lies above.
+                        const float m_sub = m == -INFINITY ? 0.f : m;
+                        const uint64_t nm2 = pack2(-m_sub, -m_sub);
+                        uint64_t ls0 = 0ull, ls1 = 0ull;
+                        float mx0 = -INFINITY, mx1 = -INFINITY;
+                        uint32_t packed[32];
+#pragma unroll
+                        for (int q = 0; q < 2; ++q)
+#pragma unroll
+                            for (int c = 0; c < 32; c += 2) {
+                                float e0, e1;
+                                unpack2(fma2(pack2(__uint_as_float(sv[q][c]), __uint_as_float(sv[q][c + 1])), sc2, nm2), e0, e1);
+                                e0 = fast_exp2(e0), e1 = fast_exp2(e1);
+                                if (c & 2) {
+                                    mx1 = max3(mx1, __uint_as_float(sv[q][c]), __uint_as_float(sv[q][c + 1]));
+                                    ls1 = add2(ls1, pack2(e0, e1));
+                                } else {
+                                    mx0 = max3(mx0, __uint_as_float(sv[q][c]), __uint_as_float(sv[q][c + 1]));
+                                    ls0 = add2(ls0, pack2(e0, e1));
+                                }
+                                packed[q * 16 + (c >> 1)] = pack_bf16(e0, e1);
+                            }
+                        if (!__any_sync(0xffffffffu, fmaxf(mx0, mx1) * kScaleLog2 > m + kRescaleThreshold)) {
+                            tmem_st32(s_addr, packed);
+                            float a0, a1, a2, a3;
+                            unpack2(ls0, a0, a1);
+                            unpack2(ls1, a2, a3);
+                            const float sum = (a0 + a2) + (a1 + a3);
+                            lu += sum;
+                            l += sum;
+                            done = true;
+                        }
+                    }
+                    if (!done) {
                     if (masked) {
 #pragma unroll
                         for (int q = 0; q < 2; ++q)
@@ -282,7 +354,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                     const float alpha = m_new == m ? 1.f : fast_exp2(m - m_new);
                     if (k > 0 && __any_sync(0xffffffffu, m_new != m)) {
                         // the accumulator as of the step before (what came before that was complete when these scores were)
-                        ok = pv_wait(steps - 1);
+                        ok = wait_all(bars + C::pv_done + 16 * x + 8 * (buf ^ 1), ((steps - 1) >> 1) & 1, s_abort);
                         if (!ok) break;
                         tc_fence_after();
                         const uint32_t o_addr = tmem + lane_addr + kColO + x * D;
@@ -301,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                     lu *= alpha;
                     m = m_new;
                     const float m_sub = m == -INFINITY ? 0.f : m;
-                    const uint64_t sc2 = pack2(kScaleLog2, kScaleLog2), nm2 = pack2(-m_sub, -m_sub);
+                    const uint64_t nm2 = pack2(-m_sub, -m_sub);
                     // (masked scores are -inf, and their weights exp2(-inf) = 0)
                     uint64_t ls0 = 0ull, ls1 = 0ull;
                     float l0 = 0.f, l1 = 0.f;
@@ -329,6 +401,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                     const float sum = (a0 + a2) + (a1 + a3);
                     lu += sum;
                     l += masked ? l0 + l1 : sum;
+                    }
                     tmem_wait_st();
                 }
                 ++steps;
@@ -340,26 +413,29 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bars + C::p_ready + 16 * buf + 8 * half);
+                if (lane == 0) mbar_arrive(bars + C::p_ready + 16 * x + 8 * buf);
             }
             if (!ok) break;
             // ---- the item's end ----
-            ok = pv_wait(steps - 1);
-            if (!ok) break;
-            tc_fence_after();
             float w0 = 1.f, w1 = 0.f;  // weights of the accumulators (streams 0 and 1 where both have a part of the row)
             int col0 = 0, col1 = D;
             uint32_t o0 = tmem + lane_addr + kColO + x * D, o1 = o0;
             if (n_x == 1) {
-                // rows of one q tile: join the streams; each writes half of the columns
                 exchange[x * kRows + t] = make_float2(m, lu);
                 rounding[x * kRows + t] = __float2half_rn(lu > 0.f ? (l - lu) / lu : 0.f);
-                tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bars + C::ex_full);
+            }
+            more = iter.next(ahead);  // (under the last PV)
+            const uint32_t last = 8 * ((steps - 1) & 1), last_par = ((steps - 1) >> 1) & 1;
+            ok = wait_all(bars + C::pv_done + 16 * x + last, last_par, s_abort);
+            if (!ok) break;
+            if (n_x == 1) {
+                // rows of one q tile: join the streams, which have taken as many steps; each writes half of the columns.  (The other's PV before
+                // its last was complete when it had the scores of its last.)
                 ok = wait_all(bars + C::ex_full, n_ex & 1, s_abort);
+                if (ok) ok = wait_all(bars + C::pv_done + 16 * (x ^ 1) + last, last_par, s_abort);
                 if (!ok) break;
-                tc_fence_after();
                 const float2 a = exchange[t], b = exchange[kRows + t];
                 const float ra = 1.f + __half2float(rounding[t]), rb = 1.f + __half2float(rounding[kRows + t]);
                 ++n_ex;
@@ -376,10 +452,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                 col0 = x * (D / 2);
                 col1 = col0 + D / 2;
             }
+            tc_fence_after();
             if (warp_valid) {
                 const bool whole = it.whole();
                 const float inv = !whole ? 1.f : l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;  // (l NaN: a score was)
                 const int head = it.head * p.G + (t & (p.G - 1));
+                char* const stage = smem + C::kOffQ + ((q_tiles + q_tile) & 1) * C::kTileBytes + (n_x == 2 ? (warp & 3) * 2 : warp) * (C::kTileBytes / 8);
                 const int slot_row = (2 * (int)blockIdx.x + (it.tile0 > 0 ? 0 : 1)) * kGroupRows + q_tile * kRows + t;
                 uint32_t flags = 0;
                 if (it.kv_len > it.tile0 * kTileKeys && it.tile1 > it.tree_tile()) {
@@ -422,18 +500,23 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                             }
                         }
                     }
-                    if (valid) {
-                        if (whole) {
-                            uint32_t y[16];
+                    if (whole) {
+                        uint32_t y[16];
 #pragma unroll
-                            for (int c = 0; c < 32; c += 2) y[c / 2] = pack_bf16(__uint_as_float(v[c]) * inv, __uint_as_float(v[c + 1]) * inv);
-                            uint4* const dst = reinterpret_cast<uint4*>(p.out + (token * p.Hq + head) * D + c0);
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) dst[k] = make_uint4(y[4 * k], y[4 * k + 1], y[4 * k + 2], y[4 * k + 3]);
+                        for (int c = 0; c < 32; c += 2) y[c / 2] = pack_bf16(__uint_as_float(v[c]) * inv, __uint_as_float(v[c + 1]) * inv);
+                        store_rows<64>(stage, lane, y, [&](int row) -> char* {
+                            const int tt = (t & ~31) + row, tok = q_tile * tile_tok + (tt >> g_shift);
+                            return tok < it.n_tok ? reinterpret_cast<char*>(p.out + (((int64_t)it.q_tok + tok) * p.Hq + it.head * p.G + (tt & (p.G - 1))) * D + c0) : nullptr;
+                        });
+                    } else {
+                        auto to = [&](int row, int c) -> char* {
+                            return q_tile * tile_tok + (((t & ~31) + row) >> g_shift) < it.n_tok ? reinterpret_cast<char*>(p.part_o + (int64_t)(slot_row - lane + row) * D + c0 + c) : nullptr;
+                        };
+                        if (D == 128) {
+                            store_rows<128>(stage, lane, v, [&](int row) { return to(row, 0); });
                         } else {
-                            uint4* const dst = reinterpret_cast<uint4*>(p.part_o + (int64_t)slot_row * D + c0);
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) dst[k] = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                            store_rows<64>(stage, lane, v, [&](int row) { return to(row, 0); });
+                            store_rows<64>(stage, lane, v + 16, [&](int row) { return to(row, 16); });
                         }
                     }
                 }
@@ -442,16 +525,17 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                     else if (p.lse) p.lse[token * p.Hq + head] = lu > 0.f ? (m + log2f(lu)) * 0.6931471805599453f : lu == 0.f ? -INFINITY : lu;
                 }
             }
-            if (n_x == 1) {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bars + C::ex_free);
+            tc_fence_before();
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                if (n_x == 1) mbar_arrive(bars + C::ex_free);
+                for (int k = 0; k < n_x; ++k) mbar_arrive(bars + C::q_empty + 8 * ((q_tiles + k) & 1));
             }
-            g += n_tiles * n_x;
+            q_tiles += n_x;
             ++n_item;
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
         if (warp == kLoadWarp) {
             // ================================================================
             // K and V tiles, in the order of use; entry e of the ring lies in slot e % kSlots
@@ -528,39 +612,22 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                     if (!more) break;
                 }
             }
-        } else if (warp == kMmaWarp) {
+        } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
             // ================================================================
-            // MMA issue.  QK^T number u (of all items: key tile by key tile, q tile by q tile) goes to buffer u & 1 once both PVs of number
-            // u - 2 have been issued; a PV takes the 64 weights of one step.
+            // MMA issue of stream x.  QK^T of a step goes to the buffer that the step before the last had, once the PV that reads its weights has
+            // been issued: the tensor pipe runs a thread's MMAs in order.
             // ================================================================
-            constexpr uint32_t kIdescQK = instr_desc(kRows, kTileKeys, false), kIdescPV = instr_desc(kRows, D, true);
+            const uint32_t x = warp - kMmaWarp;
+            constexpr uint32_t kIdescQK = instr_desc(kRows, 64, false), kIdescPV = instr_desc(kRows, D, true);
             const uint64_t desc_kmajor = smem_desc(0, 16, 1024), desc_v = smem_desc(0, C::kHalfBytes, 1024);
             PieceIter<Rows> iter_v = iter;
             Piece iv;
-            bool ok = true;
+            bool ok = true, have_k = true;
             uint32_t k_tile = 0, v_tile = 0;         // tiles that QK^T and PV have finished
-            uint32_t gk = 0, gv = 0;                 // QK^Ts issued; of them, those whose PVs have been
+            uint32_t k_steps = 0, v_steps = 0;       // steps that they have issued
             uint32_t q_tiles = 0;                    // q tiles of the items before QK^T's
-            int sk = 0, nk = 0, xk = 1;              // QK^T within the item, its number of them, its q tiles
-            int sv = 0, nv = 0, xv = 1, hv = 0;      // the same of PV, and the half
-            uint32_t pv_steps = 0;                   // bit x: parity of stream x's steps
-            bool have_k = true;
-            // which of two phases is complete first, polled for at most about the wait limit: 1, 2, or 0
-            auto either = [&](uint32_t bar1, uint32_t par1, uint32_t bar2, uint32_t par2) {
-                uint32_t t0 = 0;
-                for (uint32_t i = 1;; ++i) {
-                    if (__all_sync(0xffffffffu, mbar_test_wait(bar1, par1))) return 1;
-                    if (__all_sync(0xffffffffu, mbar_test_wait(bar2, par2))) return 2;
-                    const uint32_t limit_ns = (uint32_t)s_abort[1];
-                    if ((i & (kWaitPollsPerClockRead - 1)) == 0 || limit_ns == 0) {
-                        const uint32_t now = global_timer_lo() | 1u;
-                        if (t0 == 0) t0 = now;
-                        if (__any_sync(0xffffffffu, *s_abort || limit_ns == 0 || now - t0 > limit_ns)) break;
-                    }
-                }
-                *s_abort = 1;
-                return 0;
-            };
+            int sk = 0, nk = 0, xk = 1;              // QK^T's step within the item, the stream's number of them, the item's q tiles
+            int sv = 0, nv = 0, xv = 1;              // the same of PV
             while (ok) {
                 if (have_k && sk == nk) {
                     if (nk > 0) q_tiles += xk;
@@ -569,43 +636,51 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                     nk = have_k ? (it.tile1 - it.tile0) * xk : 0;
                     sk = 0;
                 }
-                if (gv == gk && !have_k) break;
-                const int qt = xk == 2 ? sk & 1 : 0;
-                const uint32_t ek = k_tile == 0 ? 0 : 2 * k_tile - 1, ks = ek % C::kSlots;
-                bool do_qk = have_k && gk - gv < 2;
-                if (do_qk && qt == 0) {
-                    if (gv == gk) {
+                if (v_steps == k_steps && !have_k) break;
+                const uint32_t ek = k_tile == 0 ? 0 : 2 * k_tile - 1, ks = ek % C::kSlots, vb = v_steps & 1;
+                const uint32_t qs = (q_tiles + (xk == 2 ? x : 0)) & 1;
+                bool do_qk = have_k && k_steps - v_steps < 2;
+                // (the item's Q tile may have to wait for the end of the one before, and that for its PVs)
+                const uint32_t q0 = q_tiles & 1, q0_par = (q_tiles >> 1) & 1, q1_par = ((q_tiles + 1) >> 1) & 1;
+                if (do_qk && sk == 0 && v_steps != k_steps) {
+                    const bool there = mbar_test_wait(bars + C::q_full + 8 * q0, q0_par) && (xk == 1 || mbar_test_wait(bars + C::q_full + 8 * (q0 ^ 1), q1_par));
+                    do_qk = __all_sync(0xffffffffu, there);
+                }
+                if (do_qk && (xk == 1 || (sk & 1) == 0)) {
+                    if (v_steps == k_steps) {
                         ok = wait_all(bars + C::full + 8 * ks, (ek / C::kSlots) & 1, s_abort);
                     } else {
-                        const int which = either(bars + C::full + 8 * ks, (ek / C::kSlots) & 1, bars + C::p_ready + 16 * (gv & 1) + 8 * hv, (gv >> 1) & 1);
+                        const int which = either(bars + C::full + 8 * ks, (ek / C::kSlots) & 1, bars + C::p_ready + 16 * x + 8 * vb, (v_steps >> 1) & 1);
                         ok = which != 0;
                         do_qk = which == 1;
                     }
                     if (!ok) break;
                 }
                 if (do_qk) {
-                    const uint32_t qn = q_tiles + qt, qs = qn & 1;
-                    if (sk < xk) {
-                        ok = wait_all(bars + C::q_full + 8 * qs, (qn >> 1) & 1, s_abort);
+                    const uint32_t half = xk == 2 ? sk & 1 : x;
+                    if (sk == 0) {
+                        // (both of two tiles, so that neither barrier is ever a phase behind)
+                        ok = wait_all(bars + C::q_full + 8 * q0, q0_par, s_abort);
+                        if (ok && xk == 2) ok = wait_all(bars + C::q_full + 8 * (q0 ^ 1), q1_par, s_abort);
                         if (!ok) break;
                     }
-                    const bool tile_ends = xk == 1 || qt == 1;
+                    const bool tile_ends = xk == 1 || (sk & 1) == 1;
                     tc_fence_after();
                     if (elect_one()) {
-                        const uint64_t qd = desc_kmajor + ((sbase + C::kOffQ + qs * C::kTileBytes) >> 4), kd = desc_kmajor + ((sbase + C::kOffKV + ks * C::kTileBytes) >> 4);
+                        const uint64_t qd = desc_kmajor + ((sbase + C::kOffQ + qs * C::kTileBytes) >> 4),
+                                       kd = desc_kmajor + ((sbase + C::kOffKV + ks * C::kTileBytes + half * (64 * 128)) >> 4);
 #pragma unroll
                         for (int kk = 0; kk < D / 16; ++kk) {
                             const uint32_t off = ((kk >> 2) * C::kHalfBytes + (kk & 3) * 32) >> 4;
-                            tc_mma_ss(tmem + (gk & 1) * 128, qd + off, kd + off, kIdescQK, kk > 0);
+                            tc_mma_ss(tmem + x * 128 + (k_steps & 1) * 64, qd + off, kd + off, kIdescQK, kk > 0);
                         }
-                        tc_commit(bars + C::s_full + 8 * (gk & 1));
+                        tc_commit(bars + C::s_full + 16 * x + 8 * (k_steps & 1));
                         if (tile_ends) tc_commit(bars + C::empty + 8 * ks);
-                        if (sk + xk >= nk) tc_commit(bars + C::q_empty + 8 * qs);
                     }
                     __syncwarp();
                     if (tile_ends) ++k_tile;
                     ++sk;
-                    ++gk;
+                    ++k_steps;
                     continue;
                 }
                 if (sv == nv) {
@@ -614,42 +689,59 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                     nv = (iv.tile1 - iv.tile0) * xv;
                     sv = 0;
                 }
-                const uint32_t ev = 2 * v_tile + 2, vs = ev % C::kSlots, buf = gv & 1, x = xv == 2 ? buf : hv;
-                if (hv == 0 && (xv == 1 || (sv & 1) == 0)) {
+                const uint32_t ev = 2 * v_tile + 2, vs = ev % C::kSlots, half = xv == 2 ? sv & 1 : x;
+                if (xv == 1 || (sv & 1) == 0) {
                     ok = wait_all(bars + C::full + 8 * vs, (ev / C::kSlots) & 1, s_abort);
                     if (!ok) break;
                 }
-                ok = wait_all(bars + C::p_ready + 16 * buf + 8 * hv, (gv >> 1) & 1, s_abort);
+                ok = wait_all(bars + C::p_ready + 16 * x + 8 * vb, (v_steps >> 1) & 1, s_abort);
                 if (!ok) break;
-                const bool tile_ends = hv == 1 && (xv == 1 || (sv & 1) == 1), first = xv == 2 ? sv < 2 && hv == 0 : sv == 0;
+                const bool tile_ends = xv == 1 || (sv & 1) == 1;
                 tc_fence_after();
                 if (elect_one()) {
-                    const uint64_t vd = desc_v + ((sbase + C::kOffKV + vs * C::kTileBytes) >> 4) + hv * 4 * (2048 >> 4);
+                    const uint64_t vd = desc_v + ((sbase + C::kOffKV + vs * C::kTileBytes + half * (64 * 128)) >> 4);
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk)
-                        tc_mma_ts(tmem + kColO + x * D, tmem + buf * 128 + hv * 64 + kk * 8, vd + kk * (2048 >> 4), kIdescPV, (!first || kk > 0) ? 1u : 0u);
-                    tc_commit(bars + C::pv_done + 16 * x + 8 * (pv_steps >> x & 1));
+                        tc_mma_ts(tmem + kColO + x * D, tmem + x * 128 + vb * 64 + kk * 8, vd + kk * (2048 >> 4), kIdescPV, (sv > 0 || kk > 0) ? 1u : 0u);
+                    tc_commit(bars + C::pv_done + 16 * x + 8 * vb);
                     if (tile_ends) tc_commit(bars + C::empty + 8 * vs);
                 }
                 __syncwarp();
-                pv_steps ^= 1u << x;
                 if (tile_ends) ++v_tile;
-                hv ^= 1;
-                if (hv == 0) {
-                    ++sv;
-                    ++gv;
-                }
+                ++sv;
+                ++v_steps;
             }
-        } else if (warp == kQWarp) {
+        } else {
             // ================================================================
-            // Q tiles: rows (token, head of the group) in token-major order, a box of [128 / G tokens][G heads][64 elements] per half
+            // Q tiles: rows (token, head of the group) in token-major order, a box of [128 / G tokens][G heads][64 elements] per half; and V
+            // rows that no product may read.  (Their tiles land on barriers of their own, and this warp's arrival takes the place of the
+            // copy's on the slot's.)  An item's Q may have to wait for the end of the one before, and that for its V: whichever can go on.
             // ================================================================
-            uint32_t n = 0;
-            bool ok = true;
-            while (ok && iter.next(it)) {
-                for (int x = 0; x < it.n_x(p.G) && ok; ++x, ++n) {
-                    ok = wait_all(bars + C::q_empty + 8 * (n & 1), ((n >> 1) & 1) ^ 1, s_abort);
-                    if (ok && elect_one()) {
+            PieceIter<Rows> iter_v = iter;
+            Piece iv;
+            uint32_t n = 0, v_tile = 0, n_item = 0, n_raw = 0;
+            int x = 0, n_x = 0;        // q tile of the item, of that many
+            int j = 0;                 // key tile of the item whose V comes next
+            bool ok = true, have_q = iter.next(it), have_v = iter_v.next(iv);
+            n_x = it.n_x(p.G);
+            auto begin_v = [&]() {     // to the item's first tile with tree tokens, past those that have none
+                while (have_v) {
+                    if (lane < 8) s_flagged[(n_item % C::kFlagRing) * 8 + lane] = 0u;
+                    __syncwarp();
+                    j = max(iv.tile0, iv.tree_tile());
+                    if (j < iv.tile1) return;
+                    v_tile += iv.tile1 - iv.tile0;
+                    ++n_item;
+                    have_v = iter_v.next(iv);
+                }
+            };
+            begin_v();
+            while (ok && (have_q || have_v)) {
+                const uint32_t bq = bars + C::q_empty + 8 * (n & 1), pq = ((n >> 1) & 1) ^ 1, bv = bars + C::raw + 8 * (n_raw % C::kRaw), pv = n_raw / C::kRaw & 1;
+                const int which = have_q && have_v ? either(bq, pq, bv, pv) : wait_all(have_q ? bq : bv, have_q ? pq : pv, s_abort) ? (have_q ? 1 : 2) : 0;
+                ok = which != 0;
+                if (which == 1) {
+                    if (elect_one()) {
                         mbar_expect_tx(bars + C::q_full + 8 * (n & 1), C::kTileBytes);
                         s_armed[C::kSlots + (n & 1)] = (int)((n >> 1) & 1);
 #pragma unroll
@@ -657,49 +749,43 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                             tma_load_3d(sbase + C::kOffQ + (n & 1) * C::kTileBytes + h * C::kHalfBytes, &q_map, h * 64, it.head * p.G, it.q_tok + x * tile_tok, bars + C::q_full + 8 * (n & 1));
                     }
                     __syncwarp();
-                }
-            }
-        } else {
-            // ================================================================
-            // V rows that no product may read
-            // ================================================================
-            // (they land on barriers of their own, and this warp's arrival takes the place of the copy's on the slot's)
-            uint32_t v_tile = 0, n_item = 0, n_raw = 0;
-            bool ok = true;
-            while (ok && iter.next(it)) {
-                volatile uint32_t* const flagged = s_flagged + (n_item % C::kFlagRing) * 8;
-                if (lane < 8) flagged[lane] = 0u;
-                __syncwarp();
-                for (int j = it.tile0; j < it.tile1 && ok; ++j, ++v_tile) {
-                    if (j < it.tree_tile()) continue;
-                    const uint32_t s = (2 * v_tile + 2) % C::kSlots;
-                    ok = wait_all(bars + C::raw + 8 * (n_raw % C::kRaw), n_raw / C::kRaw & 1, s_abort);
-                    if (!ok) break;
+                    ++n;
+                    if (++x == n_x) {
+                        x = 0;
+                        have_q = iter.next(it);
+                        n_x = it.n_x(p.G);
+                    }
+                } else if (which == 2) {
                     ++n_raw;
-                    for (int q = 0; q < 4; ++q) {
-                        const int key = j * kTileKeys + 32 * q + lane;
-                        char* const row = smem + C::kOffKV + s * C::kTileBytes + (32 * q + lane) * 128;
-                        bool clear = key >= it.kv_len;
-                        if (key >= it.prior && !clear) {
+                    const uint32_t s = (2 * (v_tile + j - iv.tile0) + 2) % C::kSlots;
+                    volatile uint32_t* const flagged = s_flagged + (n_item % C::kFlagRing) * 8;
+                    // (pages behind the last have landed as zeros)
+                    const int last = min((iv.kv_len + kPage - 1) / kPage * kPage, (j + 1) * kTileKeys);
+                    for (int key = max(iv.prior, j * kTileKeys) + lane; key < last; key += 32) {
+                        const int at = key & (kTileKeys - 1);
+                        char* const row = smem + C::kOffKV + s * C::kTileBytes + at * 128;
+                        bool clear = key >= iv.kv_len;
+                        if (!clear) {
 #pragma unroll
-                            for (int h = 0; h < C::kHalves; ++h)
-#pragma unroll
-                                for (int u = 0; u < 8; ++u)
-                                    clear = any_not_finite(*reinterpret_cast<const uint4*>(row + h * C::kHalfBytes + ((u ^ (lane & 7)) << 4))) || clear;
-                            if (clear) atomicOr(const_cast<uint32_t*>(flagged) + ((key - it.prior) >> 5), 1u << ((key - it.prior) & 31));
+                            for (int u = 0; u < 8 * C::kHalves; ++u)
+                                clear = any_not_finite(*reinterpret_cast<const uint4*>(row + (u >> 3) * C::kHalfBytes + (((u ^ at) & 7) << 4))) || clear;
+                            if (clear) atomicOr(const_cast<uint32_t*>(flagged) + ((key - iv.prior) >> 5), 1u << ((key - iv.prior) & 31));
                         }
                         if (clear) {
 #pragma unroll
-                            for (int h = 0; h < C::kHalves; ++h)
-#pragma unroll
-                                for (int u = 0; u < 8; ++u) *reinterpret_cast<uint4*>(row + h * C::kHalfBytes + ((u ^ (lane & 7)) << 4)) = make_uint4(0, 0, 0, 0);
+                            for (int u = 0; u < 8 * C::kHalves; ++u) *reinterpret_cast<uint4*>(row + (u >> 3) * C::kHalfBytes + ((u & 7) << 4)) = make_uint4(0, 0, 0, 0);
                         }
                     }
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bars + C::full + 8 * s);
+                    if (++j == iv.tile1) {
+                        v_tile += iv.tile1 - iv.tile0;
+                        ++n_item;
+                        have_v = iter_v.next(iv);
+                        begin_v();
+                    }
                 }
-                ++n_item;
             }
         }
     }
@@ -718,7 +804,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
             for (int x = 0; x < 2; ++x)
                 if (s_armed[C::kSlots + x] >= 0) mbar_wait(bars + C::q_full + 8 * x, (uint32_t)s_armed[C::kSlots + x], kDrainLimitNs);
         }
-        if (warp == kMmaWarp) {
+        if (warp == kMmaWarp || warp == kMmaWarp + 1) {
             if (elect_one()) tc_commit(bars + C::mma_drained);
             __syncwarp();
             mbar_wait(bars + C::mma_drained, 0, kDrainLimitNs);
@@ -738,11 +824,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
 constexpr int kMergeThreads = 256, kMergeRows = 4;  // rows of a warp
 
 template <int D, class Rows>
-__global__ void __launch_bounds__(kMergeThreads) tree_merge_kernel(const __grid_constant__ TreeParams p, int n_cta, const __grid_constant__ Rows rows) {
+__global__ void __launch_bounds__(kMergeThreads) tree_merge_kernel(const __grid_constant__ TreeParams p, const __grid_constant__ Rows rows) {
     constexpr int V = D / 32;
     pdl_trigger();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int c = (int)blockIdx.x + 1, border = share_begin(p.units, c, n_cta);
+    const int c = (int)blockIdx.x + 1, border = share_begin(p, c);
     int r;
     {
         int lo = 0, hi = p.n - 1;
@@ -758,14 +844,14 @@ __global__ void __launch_bounds__(kMergeThreads) tree_merge_kernel(const __grid_
     pdl_wait();
     // (a border at an item's begin cuts nothing, nor does one before its first tile; and the item is the first border's inside it)
     const int first_tile = begin + kItemUnits;
-    if (border <= first_tile || share_begin(p.units, c - 1, n_cta) > first_tile) return;
+    if (border <= first_tile || share_begin(p, c - 1) > first_tile) return;
     const int group_tok = kGroupRows / p.G, groups = (nodes + group_tok - 1) / group_tok;
     const int head = item / groups, tok0 = (item - head * groups) * group_tok, n_rows = min(group_tok, nodes - tok0) * p.G;
     const int row0 = ((int)blockIdx.y * (kMergeThreads / 32) + warp) * kMergeRows;
     if (row0 >= n_rows) return;
     // pieces: shares c - 1, c, ...: the first one's begins with the item, so it lies in its share's second place, the others' in the first
     int n_seg = 2;
-    while (share_begin(p.units, c + n_seg - 1, n_cta) < end) ++n_seg;
+    while (share_begin(p, c + n_seg - 1) < end) ++n_seg;
     auto place = [&](int s) { return (int64_t)(2 * (c - 1 + s) + (s == 0 ? 1 : 0)) * kGroupRows; };
     float M[kMergeRows], l[kMergeRows], lu[kMergeRows], acc[kMergeRows][V];
 #pragma unroll
@@ -880,9 +966,10 @@ ps_status launch_rows(const TreeCall& a) {
     p.wait_limit_ns = (uint32_t)a.pool->wait_limit_ns;
     p.max_pages = a.max_pages, p.mask_words = a.mask_words, p.n = a.n, p.Hq = Hq, p.Hkv = Hkv, p.G = G, p.units = (int32_t)units;
     const int grid = (int)(units / 2 < kSms ? units / 2 : kSms);  // (an item has at least two units: no share is empty)
+    p.share = (int32_t)units / grid, p.longer = (int32_t)units % grid;
     st = launch_kernel(tree_kernel<D, Rows>, grid, kThreads, Cfg<D>::kSmemBytes, a.stream, 1, true, p, q_map, pool_map, rows);
     if (st != PS_OK || grid == 1) return st;
-    return launch_kernel(tree_merge_kernel<D, Rows>, dim3(grid - 1, kGroupRows / (kMergeThreads / 32 * kMergeRows)), kMergeThreads, 0, a.stream, 1, true, p, grid, rows);
+    return launch_kernel(tree_merge_kernel<D, Rows>, dim3(grid - 1, kGroupRows / (kMergeThreads / 32 * kMergeRows)), kMergeThreads, 0, a.stream, 1, true, p, rows);
 }
 
 }  // namespace
