@@ -195,7 +195,7 @@ ps_status ps_kv_write_rope(ps_kv *kv, const ps_rope *args, const int32_t *block_
  * node that sees nothing gets zeros and lse = -inf.  What a node does not see
  * has no part in its result, whatever values it holds.
  *
- * bf16 pools.  workspace_dev: 256-byte aligned device memory of
+ * workspace_dev: 256-byte aligned device memory of
  * ps_attn_tree_workspace bytes, which depend on the shape alone; scratch, no
  * initialisation.  Calls that use one workspace are issued to one stream or
  * ordered by the caller.  Asynchronous on `stream`; may be captured into a

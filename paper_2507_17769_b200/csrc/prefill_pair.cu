@@ -940,6 +940,24 @@ ps_status encode_pool_map(const RunArgs& a, CUtensorMap* map) {
     return PS_OK;
 }
 
+ps_status encode_fp8_pool_maps(const RunArgs& a, CUtensorMap* codes, CUtensorMap* scales) {
+    EncodeTiledFn encode = tensor_map_encoder();
+    if (!encode) return fail(PS_ERR_CUDA, "the driver does not provide cuTensorMapEncodeTiled");
+    const int d = a.shape.head_dim;
+    const cuuint64_t block = fp8_page_head_bytes(d), rows = (cuuint64_t)a.num_pages * a.shape.n_kv_heads;
+    const cuuint32_t elem_strides[2] = {1, 1};
+    const cuuint64_t strides[1] = {block};
+    const cuuint64_t code_dims[2] = {block / 8, rows}, scale_dims[2] = {2 * kPage, rows};
+    const cuuint32_t code_box[2] = {(cuuint32_t)(kPage * d / 8), 1}, scale_box[2] = {2 * kPage, 1};
+    CUresult r = encode(codes, CU_TENSOR_MAP_DATA_TYPE_FLOAT64, 2, const_cast<char*>(a.pool), code_dims, strides, code_box, elem_strides,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r == CUDA_SUCCESS)
+        r = encode(scales, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<char*>(a.pool) + 2 * kPage * d, scale_dims, strides, scale_box, elem_strides,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(PS_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
+    return PS_OK;
+}
+
 ps_status launch_prefill_pair(const RunArgs& a) {
     static PerDeviceOnce configured;
     const ps_status cfg = once_per_device(configured, []() -> ps_status {

@@ -22,6 +22,9 @@ ps_status encode_q_map(const RunArgs& a, CUtensorMap* map);
 // The pool as rows of 2 KB blocks (16 tokens x 64 elements); a box is one row, gathered four at a time.
 constexpr int kPoolBlock = kPage * 128;
 ps_status encode_pool_map(const RunArgs& a, CUtensorMap* map);
+// An FP8 pool as rows of (page, kv head) blocks: boxes of 2 KB of codes (K at coordinate 0, V at 256), and of a block's 32 scales; one row, gathered
+// four at a time.
+ps_status encode_fp8_pool_maps(const RunArgs& a, CUtensorMap* codes, CUtensorMap* scales);
 
 __host__ __device__ constexpr float scale_log2(int d) { return d == 128 ? 0.12751743f : 0.18033688f; }  // log2(e) / sqrt(d)
 
@@ -53,6 +56,14 @@ __device__ __forceinline__ void tc_mma_ss(uint32_t d_tmem, uint64_t a_desc, uint
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
         "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// the same of 8-bit operands
+__device__ __forceinline__ void tc_mma_f8_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
@@ -131,6 +142,13 @@ __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.
 // Four 2 KB blocks of the pool, one after the other into shared memory (box: one row of the pool seen as rows of 2 KB; rows
 // outside the pool read as zero).  A bulk copy per block costs the issuing warp some 100 cycles each, because its operands
 // are uniform registers and the lanes take turns; with 8 of them the producers could not keep up (1500 cycles a key tile).
+__device__ __forceinline__ void gather4_at(uint32_t dst, const CUtensorMap* map, int x, int r0, int r1, int r2, int r3, uint32_t bar, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes.L2::cache_hint "
+        "[%0], [%1, {%2, %3, %4, %5, %6}], [%7], %8;" ::"r"(dst), "l"(map), "r"(x), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(bar),
+        "l"(policy)
+        : "memory");
+}
 __device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap* map, int r0, int r1, int r2, int r3, uint32_t bar, uint64_t policy) {
     asm volatile(
         "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes.L2::cache_hint "

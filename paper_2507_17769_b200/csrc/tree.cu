@@ -26,6 +26,12 @@
 //                   infinities or NaN too, because 0 * inf would reach nodes that do not see them; their weights are added by
 //                   the rows that do when the item ends.
 //
+// FP8 cache (E4M3 codes, a scale per token and kv head): half the bytes a key, so the conversion of the codes is what costs.  K's are
+// multiplied as they lie in the page: q 2^e (e of its row, the largest element in (224, 448]) is the sum of two E4M3 numbers, exactly
+// where an element has at least 2^-2 and within 2^-10 elsewhere, so S = Q1 K^T + Q2 K^T on the 8-bit tensor pipe, at the price
+// of one 16-bit product.  V's become f16, exactly; the scales multiply scores and weights in fp32, and the
+// weights are rounded to f16.  Warps 12-15 convert Q and V, in a ring of their own behind the copies'.
+//
 // Every wait is bounded; on expiry the CTA flags the pool and drains.
 #include <cuda_fp16.h>
 
@@ -35,40 +41,67 @@ namespace ps {
 
 namespace {
 
-constexpr int kThreads = 384;  // three warps a scheduler: 168 registers each
-constexpr int kLoadWarp = 8, kMmaWarp = 9;  // (MMA: 9 and 10; Q and rows of V: 11)
+constexpr int kLoadWarp = 8, kMmaWarp = 9, kQWarp = 11, kConvertWarp = 12;  // (MMA: 9 and 10)
 constexpr int kTileKeys = 128, kRows = 128;
 constexpr int kGroupRows = 2 * kRows;      // rows of an item
 constexpr int kMaxNodes = 256;
 constexpr int kItemUnits = 1;              // what an item's start and end cost, in key tiles
 constexpr float kRescaleThreshold = 8.f;   // log2 units
 
-template <int D>
+template <int D, bool FP8>
 struct Cfg {
+    static constexpr int kThreads = FP8 ? 512 : 384;         // (of three warps a scheduler each may have 168 registers)
     static constexpr int kHalves = D / 64;
     static constexpr int kHalfBytes = kTileKeys * 128;
-    static constexpr int kTileBytes = kHalves * kHalfBytes;  // a Q, K or V tile
-    static constexpr int kSlots = D == 128 ? 5 : 10;         // K and V tiles in flight
-    // Items whose flagged tree tokens are kept.  One stream may be one item ahead of the other, PV then stops, and the ring holds V tiles
-    // of kSlots / 2 + 1 items more, of a tile each.
-    static constexpr int kFlagRing = kSlots / 2 + 4;
+    static constexpr int kTileBytes = kHalves * kHalfBytes;  // a tile of Q, K or V in 16 bits
+    static constexpr int kCodeBytes = kTileKeys * D;         // of codes
+    // K and V tiles in flight: one ring in the order of their use; FP8: rings of K (codes), V (codes) and V (f16)
+    static constexpr int kSlots = FP8 ? 3 : D == 128 ? 5 : 10;
+    static constexpr int kRaw = FP8 ? 2 : kSlots / 2 + 2;    // V tiles on their way through warp 11 (more than the ring holds) or 12-15
+    static constexpr int kConv = FP8 ? 2 : 0;
+    // Tiles whose rows taken out of V are kept: an item's last three, and as many as are begun before the slower stream has written it out.
+    // (One stream may be one item ahead of the other, PV then stops, and the ring holds kSlots / 2 + 1 V tiles more.)
+    static constexpr int kFlagTiles = !FP8 && D == 64 ? 16 : 8;
+    // Tiles whose scales are kept: while the softmax works on one, K is loaded for at most four behind it.
+    static constexpr int kScaleTiles = 6, kScaleBytes = kTileKeys / kPage * 128;
     static constexpr int kOffQ = 0;                          // two tiles
     static constexpr int kOffKV = 2 * kTileBytes;
-    static constexpr int kOffBar = kOffKV + kSlots * kTileBytes;
+    static constexpr int kOffRaw = kOffKV + kSlots * (FP8 ? kCodeBytes : kTileBytes);
+    static constexpr int kOffConv = kOffRaw + (FP8 ? kRaw * kCodeBytes : 0);
+    static constexpr int kOffScale = kOffConv + kConv * kTileBytes;
+    static constexpr int kOffQScale = kOffScale + (FP8 ? kScaleTiles * kScaleBytes : 0);
+    static constexpr int kOffBar = kOffQScale + (FP8 ? 2 * kRows * 4 : 0);
     // barrier block
-    static constexpr int kRaw = kSlots / 2 + 2;              // V tiles on their way through warp 11: more than the ring holds
-    static constexpr int full = 0, empty = full + 8 * kSlots, raw = empty + 8 * kSlots;
+    static constexpr int full = 0, empty = full + 8 * kSlots, raw = empty + 8 * kSlots, raw_empty = raw + 8 * kRaw, conv_full = raw_empty + (FP8 ? 8 * kRaw : 0),
+                         conv_empty = conv_full + 8 * kConv, q_ready = conv_empty + 8 * kConv;
     // [stream][its step & 1]: scores there, weights there, product with V done
-    static constexpr int s_full = raw + 8 * kRaw, p_ready = s_full + 32, pv_done = p_ready + 32;
+    static constexpr int s_full = q_ready + (FP8 ? 16 : 0), p_ready = s_full + 32, pv_done = p_ready + 32;
     static constexpr int q_full = pv_done + 32, q_empty = q_full + 16, ex_full = q_empty + 16, ex_free = ex_full + 8, mma_drained = ex_free + 8, n_bars = (mma_drained + 8) / 8;
-    static constexpr int tmem_slot = 8 * n_bars, abort_slot = tmem_slot + 4, limit_slot = abort_slot + 4, armed = limit_slot + 4;  // slots, Q tiles, V tiles for warp 11
-    static constexpr int flagged = armed + 4 * (kSlots + 2 + kRaw);           // [item % kFlagRing][8]: tree tokens whose V row was taken out
-    static constexpr int exchange = (flagged + kFlagRing * 32 + 7) / 8 * 8;   // [stream][row] (maximum, sum of the weights)
+    static constexpr int tmem_slot = 8 * n_bars, abort_slot = tmem_slot + 4, limit_slot = abort_slot + 4, armed = limit_slot + 4;  // slots, Q tiles, raw V tiles
+    static constexpr int flagged = armed + 4 * (kSlots + 2 + kRaw);           // [tile % kFlagTiles][4]: rows taken out of V
+    static constexpr int exchange = (flagged + kFlagTiles * 16 + 7) / 8 * 8;  // [stream][row] (maximum, sum of the weights)
     static constexpr int rounding = exchange + 2 * kRows * 8;                 // [stream][row] what their rounding adds to the sum, relative, as f16
     static constexpr int bar_bytes = rounding + 2 * kRows * 2;
     static constexpr int kSmemBytes = kOffBar + bar_bytes;
     static_assert(kSmemBytes <= 232448, "shared memory");
 };
+// Where tile n of K, and of V as the products read it, lies: its barriers, their phase, its place.  16 bits: one ring in the order
+// K0 K1 V0 K2 V1 ...
+struct Slot {
+    uint32_t full, empty, par, at;
+};
+template <class C, bool FP8>
+__device__ __forceinline__ Slot ring_slot(uint32_t e) {
+    const uint32_t s = e % C::kSlots;
+    return Slot{C::full + 8 * s, C::empty + 8 * s, (e / C::kSlots) & 1, C::kOffKV + s * (FP8 ? C::kCodeBytes : C::kTileBytes)};
+}
+template <class C, bool FP8>
+__device__ __forceinline__ Slot k_slot(uint32_t n) { return ring_slot<C, FP8>(FP8 ? n : n == 0 ? 0 : 2 * n - 1); }
+template <class C, bool FP8>
+__device__ __forceinline__ Slot v_slot(uint32_t n) {
+    if (FP8) return Slot{C::conv_full + 8 * (n & 1), C::conv_empty + 8 * (n & 1), (n >> 1) & 1, C::kOffConv + (n & 1) * C::kTileBytes};
+    return ring_slot<C, FP8>(2 * n + 2);
+}
 
 // the lengths of a batch
 template <int N>
@@ -178,15 +211,28 @@ __device__ __forceinline__ void store_rows(char* stage, int lane, const uint32_t
     __syncwarp();
 }
 
+// Element e of the K (kv = 0) or V vector of a slot of a page's block
+template <int D, bool FP8>
+__device__ __forceinline__ float pool_value(const char* blk, int kv, int slot, int e) {
+    if (FP8) {
+        const uint8_t code = *reinterpret_cast<const uint8_t*>(blk + kv * kPage * D + slot * D + (((e >> 4) ^ (slot & 7)) << 4) + (e & 15));
+        uint32_t two;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(two) : "h"((uint16_t)code));
+        return __half2float(__ushort_as_half((unsigned short)two)) * reinterpret_cast<const float*>(blk + 2 * kPage * D)[kv * kPage + slot];
+    }
+    return __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(blk + kv * block_bytes(D) + unit_offset(slot, e) + 2 * (e & 7)));
+}
+
 __device__ __forceinline__ bool any_not_finite(const uint4& x) {
     auto bad = [](uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; };
     return bad(x.x) || bad(x.y) || bad(x.z) || bad(x.w);
 }
 
-template <int D, class Rows>
-__global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant__ TreeParams p, const __grid_constant__ CUtensorMap q_map,
-                                                            const __grid_constant__ CUtensorMap pool_map, const __grid_constant__ Rows rows) {
-    using C = Cfg<D>;
+template <int D, bool FP8, class Rows>
+__global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __grid_constant__ TreeParams p, const __grid_constant__ CUtensorMap q_map,
+                                                                         const __grid_constant__ CUtensorMap pool_map, const __grid_constant__ CUtensorMap scale_map,
+                                                                         const __grid_constant__ Rows rows) {
+    using C = Cfg<D, FP8>;
     extern __shared__ __align__(1024) char smem[];  // (the 128-byte swizzle wants tiles on 1024 bytes)
     const uint32_t sbase = smem_u32(smem), bars = sbase + C::kOffBar;
     volatile int* const s_abort = reinterpret_cast<volatile int*>(smem + C::kOffBar + C::abort_slot);
@@ -202,6 +248,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
             mbar_init(bars + C::empty + 8 * s, 2);
         }
         for (int s = 0; s < C::kRaw; ++s) mbar_init(bars + C::raw + 8 * s, 1);
+        if (FP8) {
+            for (int s = 0; s < C::kRaw; ++s) mbar_init(bars + C::raw_empty + 8 * s, 4);
+            for (int s = 0; s < 2; ++s) {
+                mbar_init(bars + C::conv_full + 8 * s, 4);
+                mbar_init(bars + C::conv_empty + 8 * s, 2);
+                mbar_init(bars + C::q_ready + 8 * s, 4);
+            }
+        }
         for (int k = 0; k < 4; ++k) {
             mbar_init(bars + C::s_full + 8 * k, 1);
             mbar_init(bars + C::p_ready + 8 * k, 4);
@@ -231,12 +285,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + C::kOffBar + C::tmem_slot);
     auto wait_all = [](uint32_t bar, uint32_t parity, volatile int* abort_flag) { return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag)); };
 
-    // which of two phases is complete first, polled for at most about the wait limit: 1, 2, or 0
-    auto either = [&](uint32_t bar1, uint32_t par1, uint32_t bar2, uint32_t par2) {
+    // f() until it is not 0, polled for at most about the wait limit; 0 then
+    auto poll = [&](auto f) -> int {
         uint32_t t0 = 0;
         for (uint32_t i = 1;; ++i) {
-            if (__all_sync(0xffffffffu, mbar_test_wait(bar1, par1))) return 1;
-            if (__all_sync(0xffffffffu, mbar_test_wait(bar2, par2))) return 2;
+            const int got = f();
+            if (got) return got;
             const uint32_t limit_ns = (uint32_t)s_abort[1];
             if ((i & (kWaitPollsPerClockRead - 1)) == 0 || limit_ns == 0) {
                 const uint32_t now = global_timer_lo() | 1u;
@@ -246,6 +300,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         }
         *s_abort = 1;
         return 0;
+    };
+    auto complete = [](uint32_t bar, uint32_t par) { return (bool)__all_sync(0xffffffffu, mbar_test_wait(bar, par)); };
+    // which of two phases is complete first: 1, 2, or 0
+    auto either = [&](uint32_t bar1, uint32_t par1, uint32_t bar2, uint32_t par2) {
+        return poll([&]() { return complete(bar1, par1) ? 1 : complete(bar2, par2) ? 2 : 0; });
     };
 
     constexpr uint32_t kColO = 256;
@@ -260,7 +319,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         const int x = warp >> 2, t = threadIdx.x & 127;
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
         constexpr float kScaleLog2 = scale_log2(D);
-        uint32_t steps = 0, q_tiles = 0, n_item = 0, n_ex = 0;  // of this stream; of the items before; items; exchanges
+        uint32_t steps = 0, q_tiles = 0, tiles = 0, n_ex = 0;  // of this stream; q and key tiles of the items before; exchanges
         bool ok = true, must_wait_free = false;
         Piece ahead;
         bool more = iter.next(ahead);
@@ -275,6 +334,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
             const uint32_t* const mask_row = p.mask + token * 2 * p.mask_words;
             // (the first 64 nodes' are wanted soon enough to ask for them now)
             const uint32_t mask0 = valid ? __ldg(mask_row) : 0u, mask1 = valid ? __ldg(mask_row + 1) : 0u;
+            float row_scale = kScaleLog2;            // of the scores, to log2 units
             float m = -INFINITY, l = 0.f, lu = 0.f;  // running maximum (log2 units), sums of the rounded and of the exact weights
             for (int k = 0; k < n_tiles * n_x; ++k) {
                 const int tile = n_x == 2 ? k >> 1 : k, half = n_x == 2 ? k & 1 : x;
@@ -282,6 +342,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                 ok = wait_all(bars + C::s_full + 16 * x + 8 * buf, (steps >> 1) & 1, s_abort);
                 if (!ok) break;
                 tc_fence_after();
+                if (FP8 && k == 0) row_scale = kScaleLog2 * *reinterpret_cast<const float*>(smem + C::kOffQScale + (((q_tiles + q_tile) & 1) * kRows + t) * 4);
                 if (warp_valid) {
                     const uint32_t s_addr = tmem + lane_addr + x * 128 + buf * 64;
                     const int key0 = (it.tile0 + tile) * kTileKeys + half * 64;
@@ -295,7 +356,28 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                         for (int q = 0; q < 2; ++q) vis[q] = valid ? mask_bits(mask_row, mask0, mask1, key0 + 32 * q - it.prior, it.nodes) : 0u;
                     }
                     tmem_wait_ld();
-                    const uint64_t sc2 = pack2(kScaleLog2, kScaleLog2);
+                    const uint64_t sc2 = pack2(row_scale, row_scale);
+                    // FP8: the keys' scales, 16 of K and 16 of V a page
+                    const float* const scales = reinterpret_cast<const float*>(smem + C::kOffScale + (FP8 ? (tiles + tile) % C::kScaleTiles : 0) * C::kScaleBytes) + half * 128;
+                    if (FP8) {
+#pragma unroll
+                        for (int q = 0; q < 2; ++q)
+#pragma unroll
+                            for (int c = 0; c < 32; c += 4) {
+                                const float4 ks = *reinterpret_cast<const float4*>(scales + (q * 2 + (c >> 4)) * 32 + (c & 15));
+                                sv[q][c] = __float_as_uint(__uint_as_float(sv[q][c]) * ks.x);
+                                sv[q][c + 1] = __float_as_uint(__uint_as_float(sv[q][c + 1]) * ks.y);
+                                sv[q][c + 2] = __float_as_uint(__uint_as_float(sv[q][c + 2]) * ks.z);
+                                sv[q][c + 3] = __float_as_uint(__uint_as_float(sv[q][c + 3]) * ks.w);
+                            }
+                    }
+                    // a pair of weights as PV's operand
+                    auto operand = [&](float e0, float e1, int key) -> uint32_t {
+                        if (!FP8) return pack_bf16(e0, e1);
+                        const float2 vs = *reinterpret_cast<const float2*>(scales + (key >> 4) * 32 + 16 + (key & 15));
+                        const __half2 h = __floats2half2_rn(e0 * vs.x, e1 * vs.y);
+                        return *reinterpret_cast<const uint32_t*>(&h);
+                    };
                     bool done = false;
                     if (!masked && k > 0) {
                         // Nearly every step leaves the running maximum as it is: weights and maximum at once, and again where one lies above.
@@ -318,9 +400,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                                     mx0 = max3(mx0, __uint_as_float(sv[q][c]), __uint_as_float(sv[q][c + 1]));
                                     ls0 = add2(ls0, pack2(e0, e1));
                                 }
-                                packed[q * 16 + (c >> 1)] = pack_bf16(e0, e1);
+                                packed[q * 16 + (c >> 1)] = operand(e0, e1, q * 32 + c);
                             }
-                        if (!__any_sync(0xffffffffu, fmaxf(mx0, mx1) * kScaleLog2 > m + kRescaleThreshold)) {
+                        if (!__any_sync(0xffffffffu, fmaxf(mx0, mx1) * row_scale > m + kRescaleThreshold)) {
                             tmem_st32(s_addr, packed);
                             float a0, a1, a2, a3;
                             unpack2(ls0, a0, a1);
@@ -349,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                             mx2 = max3(mx2, __uint_as_float(sv[q][c + 4]), __uint_as_float(sv[q][c + 5]));
                             mx3 = max3(mx3, __uint_as_float(sv[q][c + 6]), __uint_as_float(sv[q][c + 7]));
                         }
-                    const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * kScaleLog2;
+                    const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * row_scale;
                     const float m_new = mx > m + kRescaleThreshold ? mx : m;  // also the first finite maximum
                     const float alpha = m_new == m ? 1.f : fast_exp2(m - m_new);
                     if (k > 0 && __any_sync(0xffffffffu, m_new != m)) {
@@ -387,10 +469,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                             e0 = fast_exp2(e0), e1 = fast_exp2(e1);
                             if (c & 2) ls1 = add2(ls1, pack2(e0, e1));
                             else ls0 = add2(ls0, pack2(e0, e1));
-                            packed[q * 16 + (c >> 1)] = pack_bf16(e0, e1);
+                            uint32_t w = operand(e0, e1, q * 32 + c);
+                            if (FP8 && masked) w &= (vis[q] >> c & 1u ? 0xffffu : 0u) | (vis[q] >> c & 2u ? 0xffff0000u : 0u);  // (what lies behind the end has any scale)
+                            packed[q * 16 + (c >> 1)] = w;
                         }
                     tmem_st32(s_addr, packed);
-                    if (masked) {
+                    if (masked && !FP8) {
                         // (rows of few keys: the sum of the weights that PV multiplies keeps the output an exact mix of V rows)
 #pragma unroll
                         for (int c = 0; c < 32; ++c) l0 += bf16_lo(packed[c]), l1 += bf16_hi(packed[c]);
@@ -400,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                     unpack2(ls1, a2, a3);
                     const float sum = (a0 + a2) + (a1 + a3);
                     lu += sum;
-                    l += masked ? l0 + l1 : sum;
+                    l += masked && !FP8 ? l0 + l1 : sum;
                     }
                     tmem_wait_st();
                 }
@@ -460,9 +544,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                 char* const stage = smem + C::kOffQ + ((q_tiles + q_tile) & 1) * C::kTileBytes + (n_x == 2 ? (warp & 3) * 2 : warp) * (C::kTileBytes / 8);
                 const int slot_row = (2 * (int)blockIdx.x + (it.tile0 > 0 ? 0 : 1)) * kGroupRows + q_tile * kRows + t;
                 uint32_t flags = 0;
-                if (it.kv_len > it.tile0 * kTileKeys && it.tile1 > it.tree_tile()) {
-#pragma unroll
-                    for (int w = 0; w < kMaxNodes / 32; ++w) flags |= s_flagged[(n_item % C::kFlagRing) * 8 + w];
+                for (int j = max(it.tile0, it.tree_tile()); j < it.tile1; ++j) {
+                    const volatile uint32_t* const f = s_flagged + (tiles + j - it.tile0) % C::kFlagTiles * 4;
+                    flags |= f[0] | f[1] | f[2] | f[3];
                 }
 #pragma unroll 1
                 for (int c0 = col0; c0 < col1; c0 += 32) {
@@ -480,23 +564,20 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                     if (flags && valid) {
                         // tree tokens whose V row was taken out of the products: their weight times that row
 #pragma unroll 1
-                        for (int w = 0; w < kMaxNodes / 32; ++w) {
-                            uint32_t todo = s_flagged[(n_item % C::kFlagRing) * 8 + w] & mask_word(mask_row, min(w, 2 * p.mask_words - 1), 32 * w < it.nodes ? it.nodes : 0);
+                        for (int w = 4 * max(it.tile0, it.tree_tile()); w < 4 * it.tile1; ++w) {  // 32 keys
+                            uint32_t todo = s_flagged[(tiles + (w >> 2) - it.tile0) % C::kFlagTiles * 4 + (w & 3)] & mask_bits(mask_row, mask0, mask1, 32 * w - it.prior, it.nodes);
                             while (todo) {
-                                const int pos = it.prior + 32 * w + __ffs(todo) - 1;
+                                const int pos = 32 * w + __ffs(todo) - 1;
                                 todo &= todo - 1;
                                 const int64_t page = __ldg(p.block_table + (int64_t)it.r * p.max_pages + pos / kPage);
-                                const char* const blk = p.pool + (page * p.Hkv + it.head) * (int64_t)page_head_bytes(D);
+                                const char* const blk = p.pool + (page * p.Hkv + it.head) * (int64_t)(FP8 ? fp8_page_head_bytes(D) : page_head_bytes(D));
                                 const __nv_bfloat16* const qr = p.q + (token * p.Hq + head) * D;
                                 float dot = 0.f;
 #pragma unroll 1
-                                for (int e = 0; e < D; ++e)
-                                    dot = fmaf(__bfloat162float(qr[e]), __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(blk + unit_offset(pos % kPage, e) + 2 * (e & 7))), dot);
+                                for (int e = 0; e < D; ++e) dot = fmaf(__bfloat162float(qr[e]), pool_value<D, FP8>(blk, 0, pos % kPage, e), dot);
                                 const float weight = fast_exp2(fmaf(dot, kScaleLog2, -m));
-                                const char* const vrow = blk + block_bytes(D);
 #pragma unroll
-                                for (int c = 0; c < 32; ++c)
-                                    v[c] = __float_as_uint(fmaf(weight, __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(vrow + unit_offset(pos % kPage, c0 + c) + 2 * (c & 7))), __uint_as_float(v[c])));
+                                for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(fmaf(weight, pool_value<D, FP8>(blk, 1, pos % kPage, c0 + c), __uint_as_float(v[c])));
                             }
                         }
                     }
@@ -533,7 +614,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                 for (int k = 0; k < n_x; ++k) mbar_arrive(bars + C::q_empty + 8 * ((q_tiles + k) & 1));
             }
             q_tiles += n_x;
-            ++n_item;
+            tiles += n_tiles;
         }
     } else {
         if (warp == kLoadWarp) {
@@ -563,27 +644,44 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
             auto pool_row = [&](int page, int kv_head) {
                 const bool good = (uint32_t)page < (uint64_t)p.num_pages;
                 if (!good && page != -2 && lane < kTileKeys / kPage) atomicOr(p.flag, kStatusBounds);
-                return good ? (page * p.Hkv + kv_head) * (2 * C::kHalves) : -8;  // (rows outside the pool read as zero)
+                return good ? (page * p.Hkv + kv_head) * (FP8 ? 1 : 2 * C::kHalves) : -8;  // (rows outside the pool read as zero)
             };
             uint32_t n_raw = 0;
-            auto load = [&](int row, uint32_t e, int block, bool raw) {
+            // K (kv = 0) or V of tile n; raw: V that warp 11 looks over
+            auto load = [&](int row, uint32_t n, int kv, bool raw) {
                 int r[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    r[k] = __shfl_sync(0xffffffffu, row, k);
-                    r[k] = r[k] < 0 ? r[k] : r[k] + block;
-                }
-                const uint32_t s = e % C::kSlots, par = (e / C::kSlots) & 1;
-                if (!wait_all(bars + C::empty + 8 * s, par ^ 1, s_abort)) return false;
-                if (elect_one()) {
-                    const uint32_t land = bars + (raw ? C::raw + 8 * (n_raw % C::kRaw) : C::full + 8 * s), dst = sbase + C::kOffKV + s * C::kTileBytes;
-                    mbar_expect_tx(land, C::kTileBytes);
-                    if (raw) s_armed[C::kSlots + 2 + n_raw % C::kRaw] = (int)(n_raw / C::kRaw & 1);
-                    else s_armed[s] = (int)par;
+                for (int k = 0; k < 8; ++k) r[k] = __shfl_sync(0xffffffffu, row, k);
+                if (FP8) {
+                    const Slot at = k_slot<C, FP8>(n);
+                    const uint32_t land = kv ? C::raw + 8 * (n % C::kRaw) : at.full, free_ = kv ? C::raw_empty + 8 * (n % C::kRaw) : at.empty;
+                    const uint32_t par = kv ? (n / C::kRaw) & 1 : at.par, dst = sbase + (kv ? C::kOffRaw + n % C::kRaw * C::kCodeBytes : at.at);
+                    if (!wait_all(bars + free_, par ^ 1, s_abort)) return false;
+                    if (elect_one()) {
+                        mbar_expect_tx(bars + land, C::kCodeBytes + (kv ? 0 : C::kScaleBytes));
+                        s_armed[kv ? C::kSlots + 2 + n % C::kRaw : n % C::kSlots] = (int)par;
 #pragma unroll
-                    for (int h = 0; h < C::kHalves; ++h) {
-                        gather4(dst + h * C::kHalfBytes, &pool_map, r[0] + (r[0] < 0 ? 0 : h), r[1] + (r[1] < 0 ? 0 : h), r[2] + (r[2] < 0 ? 0 : h), r[3] + (r[3] < 0 ? 0 : h), land, policy);
-                        gather4(dst + h * C::kHalfBytes + 4 * kPoolBlock, &pool_map, r[4] + (r[4] < 0 ? 0 : h), r[5] + (r[5] < 0 ? 0 : h), r[6] + (r[6] < 0 ? 0 : h), r[7] + (r[7] < 0 ? 0 : h), land, policy);
+                        for (int k = 0; k < 8; k += 4) {
+                            gather4_at(dst + k * kPage * D, &pool_map, kv * (kPage * D / 8), r[k], r[k + 1], r[k + 2], r[k + 3], bars + land, policy);
+                            if (!kv) gather4_at(sbase + C::kOffScale + n % C::kScaleTiles * C::kScaleBytes + k * 128, &scale_map, 0, r[k], r[k + 1], r[k + 2], r[k + 3], bars + land, policy);
+                        }
+                    }
+                } else {
+                    const Slot at = kv ? v_slot<C, FP8>(n) : k_slot<C, FP8>(n);
+                    if (!wait_all(bars + at.empty, at.par ^ 1, s_abort)) return false;
+                    if (elect_one()) {
+                        const uint32_t land = bars + (raw ? C::raw + 8 * (n_raw % C::kRaw) : at.full), dst = sbase + at.at;
+                        mbar_expect_tx(land, C::kTileBytes);
+                        if (raw) s_armed[C::kSlots + 2 + n_raw % C::kRaw] = (int)(n_raw / C::kRaw & 1);
+                        else s_armed[(at.full - C::full) / 8] = (int)at.par;
+#pragma unroll
+                        for (int h = 0; h < C::kHalves; ++h) {
+                            int b[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) b[k] = r[k] < 0 ? r[k] : r[k] + kv * C::kHalves + h;
+                            gather4(dst + h * C::kHalfBytes, &pool_map, b[0], b[1], b[2], b[3], land, policy);
+                            gather4(dst + h * C::kHalfBytes + 4 * kPoolBlock, &pool_map, b[4], b[5], b[6], b[7], land, policy);
+                        }
                     }
                 }
                 __syncwarp();
@@ -604,10 +702,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                         row = pool_row(page, kv_head);
                         tree_v = tree;
                         fetch(page, kv_head, tree);
-                        ok = load(row, 2 * n + 1, 0, false);
+                        ok = load(row, n + 1, 0, false);
                         if (!ok) break;
                     }
-                    ok = load(row_v, 2 * n + 2, C::kHalves, raw);
+                    ok = load(row_v, n, 1, raw);
                     if (raw) ++n_raw;
                     if (!more) break;
                 }
@@ -618,7 +716,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
             // been issued: the tensor pipe runs a thread's MMAs in order.
             // ================================================================
             const uint32_t x = warp - kMmaWarp;
-            constexpr uint32_t kIdescQK = instr_desc(kRows, 64, false), kIdescPV = instr_desc(kRows, D, true);
+            constexpr uint32_t kQBar = FP8 ? C::q_ready : C::q_full;
+            // (FP8: E4M3 x E4M3, and f16 x f16)
+            constexpr uint32_t kTypes = (1u << 7) | (1u << 10);  // bf16 x bf16
+            constexpr uint32_t kIdescQK = instr_desc(kRows, 64, false) & (FP8 ? ~kTypes : ~0u), kIdescPV = instr_desc(kRows, D, true) & (FP8 ? ~kTypes : ~0u);
             const uint64_t desc_kmajor = smem_desc(0, 16, 1024), desc_v = smem_desc(0, C::kHalfBytes, 1024);
             PieceIter<Rows> iter_v = iter;
             Piece iv;
@@ -637,20 +738,21 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                     sk = 0;
                 }
                 if (v_steps == k_steps && !have_k) break;
-                const uint32_t ek = k_tile == 0 ? 0 : 2 * k_tile - 1, ks = ek % C::kSlots, vb = v_steps & 1;
+                const Slot ks = k_slot<C, FP8>(k_tile);
+                const uint32_t vb = v_steps & 1;
                 const uint32_t qs = (q_tiles + (xk == 2 ? x : 0)) & 1;
                 bool do_qk = have_k && k_steps - v_steps < 2;
                 // (the item's Q tile may have to wait for the end of the one before, and that for its PVs)
                 const uint32_t q0 = q_tiles & 1, q0_par = (q_tiles >> 1) & 1, q1_par = ((q_tiles + 1) >> 1) & 1;
                 if (do_qk && sk == 0 && v_steps != k_steps) {
-                    const bool there = mbar_test_wait(bars + C::q_full + 8 * q0, q0_par) && (xk == 1 || mbar_test_wait(bars + C::q_full + 8 * (q0 ^ 1), q1_par));
+                    const bool there = mbar_test_wait(bars + kQBar + 8 * q0, q0_par) && (xk == 1 || mbar_test_wait(bars + kQBar + 8 * (q0 ^ 1), q1_par));
                     do_qk = __all_sync(0xffffffffu, there);
                 }
                 if (do_qk && (xk == 1 || (sk & 1) == 0)) {
                     if (v_steps == k_steps) {
-                        ok = wait_all(bars + C::full + 8 * ks, (ek / C::kSlots) & 1, s_abort);
+                        ok = wait_all(bars + ks.full, ks.par, s_abort);
                     } else {
-                        const int which = either(bars + C::full + 8 * ks, (ek / C::kSlots) & 1, bars + C::p_ready + 16 * x + 8 * vb, (v_steps >> 1) & 1);
+                        const int which = either(bars + ks.full, ks.par, bars + C::p_ready + 16 * x + 8 * vb, (v_steps >> 1) & 1);
                         ok = which != 0;
                         do_qk = which == 1;
                     }
@@ -660,22 +762,29 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                     const uint32_t half = xk == 2 ? sk & 1 : x;
                     if (sk == 0) {
                         // (both of two tiles, so that neither barrier is ever a phase behind)
-                        ok = wait_all(bars + C::q_full + 8 * q0, q0_par, s_abort);
-                        if (ok && xk == 2) ok = wait_all(bars + C::q_full + 8 * (q0 ^ 1), q1_par, s_abort);
+                        ok = wait_all(bars + kQBar + 8 * q0, q0_par, s_abort);
+                        if (ok && xk == 2) ok = wait_all(bars + kQBar + 8 * (q0 ^ 1), q1_par, s_abort);
                         if (!ok) break;
                     }
                     const bool tile_ends = xk == 1 || (sk & 1) == 1;
                     tc_fence_after();
                     if (elect_one()) {
                         const uint64_t qd = desc_kmajor + ((sbase + C::kOffQ + qs * C::kTileBytes) >> 4),
-                                       kd = desc_kmajor + ((sbase + C::kOffKV + ks * C::kTileBytes + half * (64 * 128)) >> 4);
+                                       kd = desc_kmajor + ((sbase + ks.at + half * (64 * 128)) >> 4);
+                        const uint32_t d_tm = tmem + x * 128 + (k_steps & 1) * 64;
+                        if (FP8) {
 #pragma unroll
-                        for (int kk = 0; kk < D / 16; ++kk) {
-                            const uint32_t off = ((kk >> 2) * C::kHalfBytes + (kk & 3) * 32) >> 4;
-                            tc_mma_ss(tmem + x * 128 + (k_steps & 1) * 64, qd + off, kd + off, kIdescQK, kk > 0);
+                            for (int kk = 0; kk < 8; ++kk)  // the two parts of q, 32 elements a product
+                                tc_mma_f8_ss(d_tm, qd + (((kk >> 2) * C::kHalfBytes + (kk & 3) * 32) >> 4), kd + ((kk & 3) * 32 >> 4), kIdescQK, kk > 0);
+                        } else {
+#pragma unroll
+                            for (int kk = 0; kk < D / 16; ++kk) {
+                                const uint32_t off = ((kk >> 2) * C::kHalfBytes + (kk & 3) * 32) >> 4;
+                                tc_mma_ss(d_tm, qd + off, kd + off, kIdescQK, kk > 0);
+                            }
                         }
                         tc_commit(bars + C::s_full + 16 * x + 8 * (k_steps & 1));
-                        if (tile_ends) tc_commit(bars + C::empty + 8 * ks);
+                        if (tile_ends) tc_commit(bars + ks.empty);
                     }
                     __syncwarp();
                     if (tile_ends) ++k_tile;
@@ -689,9 +798,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                     nv = (iv.tile1 - iv.tile0) * xv;
                     sv = 0;
                 }
-                const uint32_t ev = 2 * v_tile + 2, vs = ev % C::kSlots, half = xv == 2 ? sv & 1 : x;
+                const Slot vs = v_slot<C, FP8>(v_tile);
+                const uint32_t half = xv == 2 ? sv & 1 : x;
                 if (xv == 1 || (sv & 1) == 0) {
-                    ok = wait_all(bars + C::full + 8 * vs, (ev / C::kSlots) & 1, s_abort);
+                    ok = wait_all(bars + vs.full, vs.par, s_abort);
                     if (!ok) break;
                 }
                 ok = wait_all(bars + C::p_ready + 16 * x + 8 * vb, (v_steps >> 1) & 1, s_abort);
@@ -699,39 +809,37 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                 const bool tile_ends = xv == 1 || (sv & 1) == 1;
                 tc_fence_after();
                 if (elect_one()) {
-                    const uint64_t vd = desc_v + ((sbase + C::kOffKV + vs * C::kTileBytes + half * (64 * 128)) >> 4);
+                    const uint64_t vd = desc_v + ((sbase + vs.at + half * (64 * 128)) >> 4);
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk)
                         tc_mma_ts(tmem + kColO + x * D, tmem + x * 128 + vb * 64 + kk * 8, vd + kk * (2048 >> 4), kIdescPV, (sv > 0 || kk > 0) ? 1u : 0u);
                     tc_commit(bars + C::pv_done + 16 * x + 8 * vb);
-                    if (tile_ends) tc_commit(bars + C::empty + 8 * vs);
+                    if (tile_ends) tc_commit(bars + vs.empty);
                 }
                 __syncwarp();
                 if (tile_ends) ++v_tile;
                 ++sv;
                 ++v_steps;
             }
-        } else {
+        } else if (warp == kQWarp) {
             // ================================================================
             // Q tiles: rows (token, head of the group) in token-major order, a box of [128 / G tokens][G heads][64 elements] per half; and V
             // rows that no product may read.  (Their tiles land on barriers of their own, and this warp's arrival takes the place of the
-            // copy's on the slot's.)  An item's Q may have to wait for the end of the one before, and that for its V: whichever can go on.
+            // copy's on the slot's; FP8: warps 12-15.)  An item's Q may have to wait for the end of the one before, and that for its V: whichever
+            // can go on.
             // ================================================================
             PieceIter<Rows> iter_v = iter;
             Piece iv;
-            uint32_t n = 0, v_tile = 0, n_item = 0, n_raw = 0;
+            uint32_t n = 0, v_tile = 0, n_raw = 0;
             int x = 0, n_x = 0;        // q tile of the item, of that many
             int j = 0;                 // key tile of the item whose V comes next
-            bool ok = true, have_q = iter.next(it), have_v = iter_v.next(iv);
+            bool ok = true, have_q = iter.next(it), have_v = !FP8 && iter_v.next(iv);
             n_x = it.n_x(p.G);
             auto begin_v = [&]() {     // to the item's first tile with tree tokens, past those that have none
                 while (have_v) {
-                    if (lane < 8) s_flagged[(n_item % C::kFlagRing) * 8 + lane] = 0u;
-                    __syncwarp();
                     j = max(iv.tile0, iv.tree_tile());
                     if (j < iv.tile1) return;
                     v_tile += iv.tile1 - iv.tile0;
-                    ++n_item;
                     have_v = iter_v.next(iv);
                 }
             };
@@ -757,34 +865,161 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
                     }
                 } else if (which == 2) {
                     ++n_raw;
-                    const uint32_t s = (2 * (v_tile + j - iv.tile0) + 2) % C::kSlots;
-                    volatile uint32_t* const flagged = s_flagged + (n_item % C::kFlagRing) * 8;
+                    const uint32_t n_v = v_tile + j - iv.tile0;
+                    const Slot at = v_slot<C, FP8>(n_v);
                     // (pages behind the last have landed as zeros)
-                    const int last = min((iv.kv_len + kPage - 1) / kPage * kPage, (j + 1) * kTileKeys);
-                    for (int key = max(iv.prior, j * kTileKeys) + lane; key < last; key += 32) {
-                        const int at = key & (kTileKeys - 1);
-                        char* const row = smem + C::kOffKV + s * C::kTileBytes + at * 128;
-                        bool clear = key >= iv.kv_len;
-                        if (!clear) {
+                    const int last = (iv.kv_len + kPage - 1) / kPage * kPage;
+                    for (int q = 0; q < 4; ++q) {
+                        const int row = 32 * q + lane, key = j * kTileKeys + row;
+                        char* const vrow = smem + at.at + row * 128;
+                        bool odd = false;
+                        if (key >= iv.prior && key < iv.kv_len) {
 #pragma unroll
                             for (int u = 0; u < 8 * C::kHalves; ++u)
-                                clear = any_not_finite(*reinterpret_cast<const uint4*>(row + (u >> 3) * C::kHalfBytes + (((u ^ at) & 7) << 4))) || clear;
-                            if (clear) atomicOr(const_cast<uint32_t*>(flagged) + ((key - iv.prior) >> 5), 1u << ((key - iv.prior) & 31));
+                                odd = any_not_finite(*reinterpret_cast<const uint4*>(vrow + (u >> 3) * C::kHalfBytes + (((u ^ row) & 7) << 4))) || odd;
                         }
-                        if (clear) {
+                        const uint32_t flags = __ballot_sync(0xffffffffu, odd);
+                        if (lane == 0) s_flagged[n_v % C::kFlagTiles * 4 + q] = flags;
+                        if (odd || (key >= iv.kv_len && key < last)) {
 #pragma unroll
-                            for (int u = 0; u < 8 * C::kHalves; ++u) *reinterpret_cast<uint4*>(row + (u >> 3) * C::kHalfBytes + ((u & 7) << 4)) = make_uint4(0, 0, 0, 0);
+                            for (int u = 0; u < 8 * C::kHalves; ++u) *reinterpret_cast<uint4*>(vrow + (u >> 3) * C::kHalfBytes + ((u & 7) << 4)) = make_uint4(0, 0, 0, 0);
                         }
                     }
                     fence_proxy_async_smem();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(bars + C::full + 8 * s);
+                    if (lane == 0) mbar_arrive(bars + at.full);
                     if (++j == iv.tile1) {
                         v_tile += iv.tile1 - iv.tile0;
-                        ++n_item;
                         have_v = iter_v.next(iv);
                         begin_v();
                     }
+                }
+            }
+        }
+    }
+
+    if constexpr (FP8) if (warp >= kConvertWarp) {
+        // ====================================================================
+        // FP8: q tiles into two E4M3 numbers an element, in their place, and V's codes into f16; 32 rows of each a warp, whichever tile
+        // can be worked on.  Eight lanes have a row, 16 elements each.
+        // ====================================================================
+        const int w = warp - kConvertWarp, u = lane & 7;
+        PieceIter<Rows> iter_v = iter;
+        Piece iv;
+        uint32_t n_q = 0, n_v = 0;
+        int left_q = 0, j = 0;
+        bool ok = true, have_q = iter.next(it), have_v = iter_v.next(iv);
+        left_q = it.n_x(p.G);
+        j = iv.tile0;
+        while (ok && (have_q || have_v)) {
+            const uint32_t qb = n_q & 1, vb = n_v & 1, rb = n_v % C::kRaw;
+            const int which = poll([&]() {
+                if (have_q && complete(bars + C::q_full + 8 * qb, (n_q >> 1) & 1)) return 1;
+                return have_v && complete(bars + C::raw + 8 * rb, (n_v / C::kRaw) & 1) && complete(bars + C::conv_empty + 8 * vb, ((n_v >> 1) & 1) ^ 1) ? 2 : 0;
+            });
+            ok = which != 0;
+            if (which == 1) {
+                char* const tile = smem + C::kOffQ + qb * C::kTileBytes;
+#pragma unroll 2
+                for (int i = 0; i < 8; ++i) {
+                    const int row = 32 * w + 4 * i + (lane >> 3);
+                    const char* const src = tile + (u >> 2) * C::kHalfBytes + row * 128;
+                    const uint4 a = *reinterpret_cast<const uint4*>(src + (((2 * u) ^ row) & 7) * 16), b = *reinterpret_cast<const uint4*>(src + (((2 * u + 1) ^ row) & 7) * 16);
+                    const uint32_t raw[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                    float x[16], top = 0.f;
+                    bool finite = true;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        x[2 * k] = bf16_lo(raw[k]), x[2 * k + 1] = bf16_hi(raw[k]);
+                        top = fmaxf(top, fmaxf(fabsf(x[2 * k]), fabsf(x[2 * k + 1])));
+                    }
+                    finite = !any_not_finite(a) && !any_not_finite(b);
+#pragma unroll
+                    for (int o = 4; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                    finite = (__ballot_sync(0xffffffffu, !finite) >> (lane & 24) & 0xffu) == 0;
+                    // 2^e with the row's largest times it in (224, 448]
+                    const int exponent = (int)(__float_as_uint(top) >> 23) - 127;  // (of a bf16 subnormal: -127)
+                    const bool high = (__float_as_uint(top) & 0x7fffffu) > 0x600000u;
+                    const int e = min(8 - exponent - (high ? 1 : 0), 120);
+                    const float up = __uint_as_float((uint32_t)(127 + e) << 23);
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        float y[4], rest[4];
+                        uint32_t code = 0;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            y[2 * h] = x[4 * k + 2 * h] * up, y[2 * h + 1] = x[4 * k + 2 * h + 1] * up;
+                            uint16_t two;
+                            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(y[2 * h + 1]), "f"(y[2 * h]));
+                            code |= (uint32_t)two << (16 * h);
+                            uint32_t back;
+                            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(back) : "h"(two));
+                            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&back));
+                            rest[2 * h] = y[2 * h] - f.x, rest[2 * h + 1] = y[2 * h + 1] - f.y;
+                        }
+                        hi[k] = code;
+                        uint16_t r0, r1;
+                        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r0) : "f"(rest[1]), "f"(rest[0]));
+                        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r1) : "f"(rest[3]), "f"(rest[2]));
+                        lo[k] = (uint32_t)r0 | (uint32_t)r1 << 16;
+                    }
+                    __syncwarp();  // (the row's other lanes have read what is overwritten)
+                    char* const dst = tile + row * 128 + (((u ^ row) & 7) << 4);
+                    *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                    *reinterpret_cast<uint4*>(dst + C::kHalfBytes) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                    if (u == 0) *reinterpret_cast<float*>(smem + C::kOffQScale + (qb * kRows + row) * 4) = finite ? __uint_as_float((uint32_t)(127 - e) << 23) : __uint_as_float(0x7fffffffu);
+                    __syncwarp();
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bars + C::q_ready + 8 * qb);
+                ++n_q;
+                if (--left_q == 0) {
+                    have_q = iter.next(it);
+                    left_q = it.n_x(p.G);
+                }
+            } else if (which == 2) {
+                const bool tree = j >= iv.tree_tile();
+                const char* const src = smem + C::kOffRaw + rb * C::kCodeBytes;
+                char* const dst = smem + C::kOffConv + vb * C::kTileBytes + (u >> 2) * C::kHalfBytes;
+                uint32_t flags = 0;
+#pragma unroll 2
+                for (int i = 0; i < 8; ++i) {
+                    const int row = 32 * w + 4 * i + (lane >> 3), key = j * kTileKeys + row;
+                    uint4 code = *reinterpret_cast<const uint4*>(src + row * 128 + (((u ^ row) & 7) << 4));
+                    if (tree) {
+                        auto nan = [](uint32_t c) { return (((c & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0; };
+                        const bool odd = key >= iv.prior && key < iv.kv_len && (nan(code.x) || nan(code.y) || nan(code.z) || nan(code.w));
+                        const uint32_t any = __ballot_sync(0xffffffffu, odd);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) flags |= (any >> (8 * k) & 0xffu ? 1u : 0u) << (4 * i + k);
+                        if (key >= iv.kv_len || (any >> (lane & 24) & 0xffu)) code = make_uint4(0, 0, 0, 0);
+                    }
+                    const uint32_t c[4] = {code.x, code.y, code.z, code.w};
+                    uint32_t y[8];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * k]) : "h"((uint16_t)c[k]));
+                        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * k + 1]) : "h"((uint16_t)(c[k] >> 16)));
+                    }
+                    // (the halves' lanes begin at different units: no bank conflicts)
+                    const bool swap = u & 4;
+                    const int u0 = 2 * u + (swap ? 1 : 0), u1 = 2 * u + (swap ? 0 : 1);
+                    *reinterpret_cast<uint4*>(dst + row * 128 + (((u0 ^ row) & 7) << 4)) = swap ? make_uint4(y[4], y[5], y[6], y[7]) : make_uint4(y[0], y[1], y[2], y[3]);
+                    *reinterpret_cast<uint4*>(dst + row * 128 + (((u1 ^ row) & 7) << 4)) = swap ? make_uint4(y[0], y[1], y[2], y[3]) : make_uint4(y[4], y[5], y[6], y[7]);
+                }
+                if (tree && lane == 0) s_flagged[n_v % C::kFlagTiles * 4 + w] = flags;
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(bars + C::conv_full + 8 * vb);
+                    mbar_arrive(bars + C::raw_empty + 8 * rb);
+                }
+                ++n_v;
+                if (++j == iv.tile1) {
+                    have_v = iter_v.next(iv);
+                    j = iv.tile0;
                 }
             }
         }
@@ -914,7 +1149,7 @@ struct TreeCall {
     cudaStream_t stream;
 };
 
-template <int D, int N>
+template <int D, bool FP8, int N>
 ps_status launch_rows(const TreeCall& a) {
     const ps_shape& shape = a.pool->shape;
     const int Hq = shape.n_q_heads, Hkv = shape.n_kv_heads, G = Hq / Hkv, group_tok = kGroupRows / G;
@@ -938,7 +1173,7 @@ ps_status launch_rows(const TreeCall& a) {
 
     static PerDeviceOnce configured;
     const ps_status cfg = once_per_device(configured, []() -> ps_status {
-        PS_CUDA_TRY(cudaFuncSetAttribute(tree_kernel<D, Rows>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::kSmemBytes));
+        PS_CUDA_TRY(cudaFuncSetAttribute(tree_kernel<D, FP8, Rows>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, FP8>::kSmemBytes));
         return PS_OK;
     });
     if (cfg != PS_OK) return cfg;
@@ -948,9 +1183,10 @@ ps_status launch_rows(const TreeCall& a) {
     m.num_pages = a.pool->num_pages;
     m.q = (const __nv_bfloat16*)a.q;
     m.total_q = tokens;
-    CUtensorMap q_map, pool_map;
+    CUtensorMap q_map, pool_map, scale_map;
     ps_status st = encode_q_map(m, &q_map);
-    if (st == PS_OK) st = encode_pool_map(m, &pool_map);
+    if (st == PS_OK) st = FP8 ? encode_fp8_pool_maps(m, &pool_map, &scale_map) : encode_pool_map(m, &pool_map);
+    if (!FP8) scale_map = pool_map;  // (not used)
     if (st != PS_OK) return st;
     TreeParams p{};
     p.q = m.q;
@@ -967,7 +1203,7 @@ ps_status launch_rows(const TreeCall& a) {
     p.max_pages = a.max_pages, p.mask_words = a.mask_words, p.n = a.n, p.Hq = Hq, p.Hkv = Hkv, p.G = G, p.units = (int32_t)units;
     const int grid = (int)(units / 2 < kSms ? units / 2 : kSms);  // (an item has at least two units: no share is empty)
     p.share = (int32_t)units / grid, p.longer = (int32_t)units % grid;
-    st = launch_kernel(tree_kernel<D, Rows>, grid, kThreads, Cfg<D>::kSmemBytes, a.stream, 1, true, p, q_map, pool_map, rows);
+    st = launch_kernel(tree_kernel<D, FP8, Rows>, grid, Cfg<D, FP8>::kThreads, Cfg<D, FP8>::kSmemBytes, a.stream, 1, true, p, q_map, pool_map, scale_map, rows);
     if (st != PS_OK || grid == 1) return st;
     return launch_kernel(tree_merge_kernel<D, Rows>, dim3(grid - 1, kGroupRows / (kMergeThreads / 32 * kMergeRows)), kMergeThreads, 0, a.stream, 1, true, p, rows);
 }
@@ -995,7 +1231,6 @@ ps_status ps_attn_tree(const ps_kv* kv, const void* q_dev, const int32_t* block_
     if (n < 1 || max_pages < 1) return fail(PS_ERR_INVALID, "n=%d, max_pages=%d must be positive", n, max_pages);
     if (mask_words < 1 || mask_words > kMaxNodes / 64) return fail(PS_ERR_UNSUPPORTED, "mask_words=%d: masks of 1 to %d words are supported", mask_words, kMaxNodes / 64);
     const KvPool& pool = pool_of(kv);
-    if (pool.shape.dtype != 0) return fail(PS_ERR_UNSUPPORTED, "tree attention is supported on bf16 pools only");
     if (workspace_bytes_given < workspace_bytes(pool.shape))
         return fail(PS_ERR_WORKSPACE, "workspace has %zu bytes, tree attention needs %zu", workspace_bytes_given, workspace_bytes(pool.shape));
     if ((uintptr_t)workspace_dev % 256 != 0) return fail(PS_ERR_INVALID, "workspace must be 256-byte aligned");
@@ -1015,8 +1250,9 @@ ps_status ps_attn_tree(const ps_kv* kv, const void* q_dev, const int32_t* block_
         const TreeCall a{&pool, (const char*)q_dev + t0 * row * 2, block_table_dev + (int64_t)r0 * max_pages, max_pages, mask_dev + t0 * mask_words, mask_words, prior_host + r0,
                          n_nodes_host + r0, m, (char*)out_dev + t0 * row * 2, lse_out_dev ? lse_out_dev + t0 * pool.shape.n_q_heads : nullptr, (char*)workspace_dev,
                          (cudaStream_t)stream};
-        const ps_status st = pool.shape.head_dim == 128 ? (m <= 64 ? launch_rows<128, 64>(a) : m <= 512 ? launch_rows<128, 512>(a) : launch_rows<128, kTreeRowsMax>(a))
-                                                        : (m <= 64 ? launch_rows<64, 64>(a) : m <= 512 ? launch_rows<64, 512>(a) : launch_rows<64, kTreeRowsMax>(a));
+        const ps_status st = pool.shape.dtype == 1        ? (m <= 64 ? launch_rows<128, true, 64>(a) : m <= 512 ? launch_rows<128, true, 512>(a) : launch_rows<128, true, kTreeRowsMax>(a))
+                             : pool.shape.head_dim == 128 ? (m <= 64 ? launch_rows<128, false, 64>(a) : m <= 512 ? launch_rows<128, false, 512>(a) : launch_rows<128, false, kTreeRowsMax>(a))
+                                                          : (m <= 64 ? launch_rows<64, false, 64>(a) : m <= 512 ? launch_rows<64, false, 512>(a) : launch_rows<64, false, kTreeRowsMax>(a));
         if (st != PS_OK) return st;
         for (int32_t r = r0; r < r0 + m; ++r) t0 += n_nodes_host[r];
     }

@@ -77,7 +77,10 @@ def tree_reference(cache, q, prior, sees_all):
     Bounds.  The weights that multiply V are rounded to bf16 (2^-8 of each), and so is their sum's share of that where it is taken
     over the rounded ones: 2 * 2^-8 of sum |w v|.  The output's own rounding: 2^-8 of it.  A score is a sum of d products in
     fp32: d * 2^-24 * sum |q k| / sqrt(d); twice that relative in the weights (numerator and sum), once absolute in lse;
-    ex2.approx and the logarithm are good to 2^-20, the sums to 2^-18 over the lengths here."""
+    ex2.approx and the logarithm are good to 2^-20, the sums to 2^-18 over the lengths here.
+    FP8 cache: the weights times their scales are rounded to f16 (2^-11, and 2^-24 at the least, of values up to 2^8 times V's largest scale); q is the
+    sum of two E4M3 numbers over a power of two that brings a row's largest to 224 at least, off by at most half of their smallest
+    step, 2^-10; its products are twice as many."""
     outs, lses, bounds, lse_bounds, t = [], [], [], [], 0
     d, group = cache.dim, cache.heads // cache.kv_heads
     for r, sees in enumerate(sees_all):
@@ -99,10 +102,16 @@ def tree_reference(cache, q, prior, sees_all):
             part = torch.where(hidden[:, key][None, :, None], 0.0, w[:, :, key, None] * (v - fin)[:, key][:, None])
             out = out + torch.where(hidden[:, key][None, :, None] | torch.isfinite(v[:, key])[:, None], 0.0, part)
         weight = w @ fin.abs()
-        score = (d * 2.0 ** -24 / math.sqrt(d)) * (x.abs() @ torch.nan_to_num(k, 0, 0, 0).abs().transpose(1, 2)).masked_fill(hidden, 0).amax(-1)
+        mag = torch.nan_to_num(k, 0, 0, 0).abs().transpose(1, 2)
+        score = (d * 2.0 ** -24 / math.sqrt(d)) * (x.abs() @ mag).masked_fill(hidden, 0).amax(-1)
+        rounding = 2.0 ** -7
+        if cache.fp8:
+            split = x.abs().amax(-1, keepdim=True) * (2.0 ** -10 / 224)
+            score = 2 * score + (split.expand_as(x) @ mag).masked_fill(hidden, 0).amax(-1) / math.sqrt(d)
+            rounding = 2.0 ** -11
         outs.append(out.transpose(0, 1))
         lses.append(lse.transpose(0, 1))
-        bounds.append((2.0 ** -8 * out.abs() + (2.0 ** -7 + 2 * score[..., None] + 2.0 ** -18) * weight).transpose(0, 1))
+        bounds.append((2.0 ** -8 * out.abs() + (rounding + 2 * score[..., None] + 2.0 ** -18) * weight + (2.0 ** -13 if cache.fp8 else 0.0)).transpose(0, 1))
         lse_bounds.append((score + 2.0 ** -18 + 2.0 ** -22 * torch.nan_to_num(lse, 0, 0, 0).abs()).transpose(0, 1))
         t += n
     return torch.cat(outs), torch.cat(lses), torch.cat(bounds), torch.cat(lse_bounds)

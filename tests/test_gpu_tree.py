@@ -9,13 +9,13 @@ pytestmark = pytest.mark.gpu
 HEADS = [(32, 8, 128), (8, 8, 128), (16, 2, 128), (2, 1, 128), (8, 8, 64), (4, 2, 64), (32, 4, 64)]
 
 
-def run(heads, prior, nodes, seed=0, words=None, q_scale=1.0, sees_all=None):
+def run(heads, prior, nodes, seed=0, words=None, q_scale=1.0, sees_all=None, fp8=False):
     import torch
 
     rng = np.random.default_rng(seed)
     prior, nodes = np.asarray(prior, dtype=np.int32), np.asarray(nodes, dtype=np.int32)
     words = words or (int(nodes.max()) + 63) // 64
-    cache = Cache(*heads, prior + nodes, seed=seed).fill()
+    cache = Cache(*heads, prior + nodes, seed=seed, fp8=fp8).fill()
     mask, sees = tree_masks(nodes, words, rng)
     if sees_all is not None:
         sees, mask = sees_all, torch.from_numpy(np.concatenate([pack(s, words) for s in sees_all])).cuda()
