@@ -29,8 +29,9 @@
 // FP8 cache (E4M3 codes, a scale per token and kv head): half the bytes a key, so the conversion of the codes is what costs.  K's are
 // multiplied as they lie in the page: q 2^e (e of its row, the largest element in (224, 448]) is the sum of two E4M3 numbers, exactly
 // where an element has at least 2^-2 and within 2^-10 elsewhere, so S = Q1 K^T + Q2 K^T on the 8-bit tensor pipe, at the price
-// of one 16-bit product.  V's become f16, exactly; the scales multiply scores and weights in fp32, and the
-// weights are rounded to f16.  Warps 12-15 convert Q and V, in a ring of their own behind the copies'.
+// of one 16-bit product.  K's scales multiply the scores in fp32.  V becomes f16, code times half the scale (11 of at most 12 significant
+// bits; half, so that scales up to 255 stay in range), and the weights are rounded to f16.  Warp 11 converts Q, warps 12-15 V,
+// in a ring of its own behind the copies'.
 //
 // Every wait is bounded; on expiry the CTA flags the pool and drains.
 #include <cuda_fp16.h>
@@ -70,7 +71,9 @@ struct Cfg {
     static constexpr int kOffConv = kOffRaw + (FP8 ? kRaw * kCodeBytes : 0);
     static constexpr int kOffScale = kOffConv + kConv * kTileBytes;
     static constexpr int kOffQScale = kOffScale + (FP8 ? kScaleTiles * kScaleBytes : 0);
-    static constexpr int kOffBar = kOffQScale + (FP8 ? 2 * kRows * 4 : 0);
+    static constexpr int kOffRawScale = kOffQScale + (FP8 ? 2 * kRows * 4 : 0);  // with V's codes
+    static constexpr int kOffPieces = kOffRawScale + (FP8 ? kRaw * kScaleBytes : 0);  // [softmax warp][2]
+    static constexpr int kOffBar = kOffPieces + (FP8 ? 8 * 2 * 48 : 0);
     // barrier block
     static constexpr int full = 0, empty = full + 8 * kSlots, raw = empty + 8 * kSlots, raw_empty = raw + 8 * kRaw, conv_full = raw_empty + (FP8 ? 8 * kRaw : 0),
                          conv_empty = conv_full + 8 * kConv, q_ready = conv_empty + 8 * kConv;
@@ -80,8 +83,7 @@ struct Cfg {
     static constexpr int tmem_slot = 8 * n_bars, abort_slot = tmem_slot + 4, limit_slot = abort_slot + 4, armed = limit_slot + 4;  // slots, Q tiles, raw V tiles
     static constexpr int flagged = armed + 4 * (kSlots + 2 + kRaw);           // [tile % kFlagTiles][4]: rows taken out of V
     static constexpr int exchange = (flagged + kFlagTiles * 16 + 7) / 8 * 8;  // [stream][row] (maximum, sum of the weights)
-    static constexpr int rounding = exchange + 2 * kRows * 8;                 // [stream][row] what their rounding adds to the sum, relative, as f16
-    static constexpr int bar_bytes = rounding + 2 * kRows * 2;
+    static constexpr int bar_bytes = exchange + 2 * kRows * 8;
     static constexpr int kSmemBytes = kOffBar + bar_bytes;
     static_assert(kSmemBytes <= 232448, "shared memory");
 };
@@ -117,7 +119,7 @@ struct TreeParams {
     const char* pool;
     __nv_bfloat16* out;
     float* lse;
-    float4* part_ml;        // [2 CTAs][256 rows]
+    float2* part_ml;        // [2 CTAs][256 rows]: maximum (log2 units), sum of the weights
     float* part_o;
     int* flag;
     int64_t num_pages;
@@ -127,7 +129,7 @@ struct TreeParams {
 
 // pieces of items in a CTA's share of the line
 struct Piece {
-    int r, head, q_tok, n_tok, tok0, nodes, prior, kv_len;
+    int r, head, q_tok, n_tok, nodes, prior, kv_len;  // (the group's tokens)
     int tile0, tile1, tiles;
     __device__ __forceinline__ int n_x(int G) const { return n_tok * G > kRows ? 2 : 1; }
     __device__ __forceinline__ bool whole() const { return tile0 == 0 && tile1 == tiles; }
@@ -136,38 +138,51 @@ struct Piece {
 };
 __device__ __forceinline__ int share_begin(const TreeParams& p, int c) { return c * p.share + min(c, p.longer); }
 
+// (What is common to the roles is short: their code shares the SM's instruction cache, which all of it together overflows.)
 template <class Rows>
 struct PieceIter {
     const Rows& rows;
-    int n, G, u, end, r;
-    __device__ __forceinline__ PieceIter(const Rows& rows_, int n_, int G_, int u_, int end_) : rows(rows_), n(n_), G(G_), u(u_), end(end_) {
+    int G, Hkv, left, r, head, group, w0;  // units left of the share; where it goes on: request, kv head, group, units into the item
+    __device__ __forceinline__ int tiles() const { return (rows.prior[r] + rows.q_start[r + 1] - rows.q_start[r] + kTileKeys - 1) / kTileKeys; }
+    __device__ __forceinline__ int groups(int nodes) const {
+        const int shift = 31 - __clz(kGroupRows / G);  // (G is a power of two)
+        return (nodes + (1 << shift) - 1) >> shift;
+    }
+    __device__ __forceinline__ PieceIter(const Rows& rows_, int n, int G_, int Hkv_, int u, int end) : rows(rows_), G(G_), Hkv(Hkv_), left(end - u) {
         int lo = 0, hi = n - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (rows.unit_start[mid] <= u) lo = mid; else hi = mid - 1;
         }
         r = lo;
+        const int per = tiles() + kItemUnits, o = u - rows.unit_start[r], item = o / per, gr = groups(rows.q_start[r + 1] - rows.q_start[r]);
+        w0 = o - item * per;
+        head = item / gr;
+        group = item - head * gr;
     }
     __device__ __forceinline__ bool next(Piece& x) {
-        while (u < end) {
-            while (u >= rows.unit_start[r + 1]) ++r;
+        while (left > 0) {
             x.r = r;
             x.prior = rows.prior[r];
             x.q_tok = rows.q_start[r];
             x.nodes = rows.q_start[r + 1] - x.q_tok;
             x.kv_len = x.prior + x.nodes;
-            x.tiles = (x.kv_len + kTileKeys - 1) / kTileKeys;
-            const int per = x.tiles + kItemUnits, o = u - rows.unit_start[r], item = o / per, w0 = o - item * per, w1 = min(per, w0 + end - u);
-            u += w1 - w0;
+            x.tiles = tiles();
+            x.head = head;
             x.tile0 = max(0, w0 - kItemUnits);
-            x.tile1 = max(0, w1 - kItemUnits);
-            if (x.tile1 <= x.tile0) continue;
-            const int shift = 31 - __clz(kGroupRows / G), group_tok = 1 << shift, groups = (x.nodes + group_tok - 1) >> shift;  // (G is a power of two)
-            x.head = groups == 1 ? item : item / groups;
-            x.tok0 = (item - x.head * groups) * group_tok;
-            x.n_tok = min(group_tok, x.nodes - x.tok0);
-            x.q_tok += x.tok0;
-            return true;
+            x.tile1 = max(0, min(x.tiles + kItemUnits, w0 + left) - kItemUnits);
+            left -= x.tiles + kItemUnits - w0;
+            w0 = 0;
+            const int tok0 = group * (kGroupRows / G);
+            x.n_tok = min(kGroupRows / G, x.nodes - tok0);
+            x.q_tok += tok0;
+            if (tok0 + x.n_tok == x.nodes) {
+                group = 0;
+                if (++head == Hkv) head = 0, ++r;
+            } else {
+                ++group;
+            }
+            if (x.tile1 > x.tile0) return true;
         }
         return false;
     }
@@ -223,6 +238,11 @@ __device__ __forceinline__ float pool_value(const char* blk, int kv, int slot, i
     return __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(blk + kv * block_bytes(D) + unit_offset(slot, e) + 2 * (e & 7)));
 }
 
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
 __device__ __forceinline__ bool any_not_finite(const uint4& x) {
     auto bad = [](uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; };
     return bad(x.x) || bad(x.y) || bad(x.z) || bad(x.w);
@@ -239,7 +259,6 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
     volatile int* const s_armed = reinterpret_cast<volatile int*>(smem + C::kOffBar + C::armed);  // (-1: never; read only after an abort)
     volatile uint32_t* const s_flagged = reinterpret_cast<volatile uint32_t*>(smem + C::kOffBar + C::flagged);
     float2* const exchange = reinterpret_cast<float2*>(smem + C::kOffBar + C::exchange);
-    __half* const rounding = reinterpret_cast<__half*>(smem + C::kOffBar + C::rounding);
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
@@ -253,7 +272,7 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
             for (int s = 0; s < 2; ++s) {
                 mbar_init(bars + C::conv_full + 8 * s, 4);
                 mbar_init(bars + C::conv_empty + 8 * s, 2);
-                mbar_init(bars + C::q_ready + 8 * s, 4);
+                mbar_init(bars + C::q_ready + 8 * s, 1);
             }
         }
         for (int k = 0; k < 4; ++k) {
@@ -285,14 +304,16 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + C::kOffBar + C::tmem_slot);
     auto wait_all = [](uint32_t bar, uint32_t parity, volatile int* abort_flag) { return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag)); };
 
-    // f() until it is not 0, polled for at most about the wait limit; 0 then
-    auto poll = [&](auto f) -> int {
+    // f() until it is not 0, polled for at most about the wait limit; 0 then.  (Between polls the warp sleeps: every question takes
+    // its turn in the queue that the other warps' shared-memory accesses go through.)
+    auto poll = [&](uint32_t sleep_ns, auto f) -> int {
         uint32_t t0 = 0;
         for (uint32_t i = 1;; ++i) {
             const int got = f();
             if (got) return got;
+            __nanosleep(sleep_ns);
             const uint32_t limit_ns = (uint32_t)s_abort[1];
-            if ((i & (kWaitPollsPerClockRead - 1)) == 0 || limit_ns == 0) {
+            if ((i & 15) == 0 || limit_ns == 0) {
                 const uint32_t now = global_timer_lo() | 1u;
                 if (t0 == 0) t0 = now;
                 if (__any_sync(0xffffffffu, *s_abort || limit_ns == 0 || now - t0 > limit_ns)) break;
@@ -303,12 +324,12 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
     };
     auto complete = [](uint32_t bar, uint32_t par) { return (bool)__all_sync(0xffffffffu, mbar_test_wait(bar, par)); };
     // which of two phases is complete first: 1, 2, or 0
-    auto either = [&](uint32_t bar1, uint32_t par1, uint32_t bar2, uint32_t par2) {
-        return poll([&]() { return complete(bar1, par1) ? 1 : complete(bar2, par2) ? 2 : 0; });
+    auto either = [&](uint32_t sleep_ns, uint32_t bar1, uint32_t par1, uint32_t bar2, uint32_t par2) {
+        return poll(sleep_ns, [&]() { return complete(bar1, par1) ? 1 : complete(bar2, par2) ? 2 : 0; });
     };
 
     constexpr uint32_t kColO = 256;
-    PieceIter<Rows> iter(rows, p.n, p.G, share_begin(p, blockIdx.x), share_begin(p, blockIdx.x + 1));
+    PieceIter<Rows> iter(rows, p.n, p.G, p.Hkv, share_begin(p, blockIdx.x), share_begin(p, blockIdx.x + 1));
     Piece it;
     const int tile_tok = kRows / p.G, g_shift = 31 - __clz(p.G);
 
@@ -321,10 +342,28 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
         constexpr float kScaleLog2 = scale_log2(D);
         uint32_t steps = 0, q_tiles = 0, tiles = 0, n_ex = 0;  // of this stream; q and key tiles of the items before; exchanges
         bool ok = true, must_wait_free = false;
+        // FP8: the pieces wait in shared memory, for want of registers beside a step's scores
         Piece ahead;
         bool more = iter.next(ahead);
+        uint32_t n_piece = 0;
+        int* const kept = reinterpret_cast<int*>(smem + C::kOffPieces + warp * 96);
+        auto keep = [&](uint32_t n, const Piece& a) {
+            if (FP8 && lane == 0) {
+                int* const to = kept + (n & 1) * 12;
+                to[0] = a.r, to[1] = a.head, to[2] = a.q_tok, to[3] = a.n_tok, to[4] = a.nodes, to[5] = a.prior, to[6] = a.kv_len, to[7] = a.tile0, to[8] = a.tile1, to[9] = a.tiles;
+            }
+            __syncwarp();
+        };
+        auto kept_piece = [&](uint32_t n) {
+            const volatile int* const from = kept + (n & 1) * 12;
+            Piece a;
+            a.r = from[0], a.head = from[1], a.q_tok = from[2], a.n_tok = from[3], a.nodes = from[4], a.prior = from[5], a.kv_len = from[6], a.tile0 = from[7], a.tile1 = from[8], a.tiles = from[9];
+            return a;
+        };
+        if (more) keep(0, ahead);
         while (ok && more) {
-            it = ahead;
+            if (FP8) it = kept_piece(n_piece);
+            else it = ahead;
             const int n_x = it.n_x(p.G), n_tiles = it.tile1 - it.tile0;
             const int q_tile = n_x == 2 ? x : 0;
             const int row_tok = q_tile * tile_tok + (t >> g_shift);  // token of this row within the item
@@ -335,7 +374,7 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
             // (the first 64 nodes' are wanted soon enough to ask for them now)
             const uint32_t mask0 = valid ? __ldg(mask_row) : 0u, mask1 = valid ? __ldg(mask_row + 1) : 0u;
             float row_scale = kScaleLog2;            // of the scores, to log2 units
-            float m = -INFINITY, l = 0.f, lu = 0.f;  // running maximum (log2 units), sums of the rounded and of the exact weights
+            float m = -INFINITY, l = 0.f;            // running maximum (log2 units), sum of the weights
             for (int k = 0; k < n_tiles * n_x; ++k) {
                 const int tile = n_x == 2 ? k >> 1 : k, half = n_x == 2 ? k & 1 : x;
                 const uint32_t buf = steps & 1;
@@ -347,79 +386,77 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                     const uint32_t s_addr = tmem + lane_addr + x * 128 + buf * 64;
                     const int key0 = (it.tile0 + tile) * kTileKeys + half * 64;
                     const bool masked = key0 + 64 > it.prior;
-                    uint32_t sv[2][32];
-                    tmem_ld32(s_addr, sv[0]);
-                    tmem_ld32(s_addr + 32, sv[1]);
-                    uint32_t vis[2];
-                    if (masked) {
-#pragma unroll
-                        for (int q = 0; q < 2; ++q) vis[q] = valid ? mask_bits(mask_row, mask0, mask1, key0 + 32 * q - it.prior, it.nodes) : 0u;
-                    }
-                    tmem_wait_ld();
                     const uint64_t sc2 = pack2(row_scale, row_scale);
-                    // FP8: the keys' scales, 16 of K and 16 of V a page
-                    const float* const scales = reinterpret_cast<const float*>(smem + C::kOffScale + (FP8 ? (tiles + tile) % C::kScaleTiles : 0) * C::kScaleBytes) + half * 128;
-                    if (FP8) {
+                    // FP8: times the keys' scales, 16 of K and 16 of V a page
+                    const float* const scales = reinterpret_cast<const float*>(smem + C::kOffScale + (tiles + tile) % C::kScaleTiles * C::kScaleBytes) + half * 128;
+                    auto scaled = [&](uint32_t (&sv)[32], int q) {
+                        if (!FP8) return;
 #pragma unroll
-                        for (int q = 0; q < 2; ++q)
-#pragma unroll
-                            for (int c = 0; c < 32; c += 4) {
-                                const float4 ks = *reinterpret_cast<const float4*>(scales + (q * 2 + (c >> 4)) * 32 + (c & 15));
-                                sv[q][c] = __float_as_uint(__uint_as_float(sv[q][c]) * ks.x);
-                                sv[q][c + 1] = __float_as_uint(__uint_as_float(sv[q][c + 1]) * ks.y);
-                                sv[q][c + 2] = __float_as_uint(__uint_as_float(sv[q][c + 2]) * ks.z);
-                                sv[q][c + 3] = __float_as_uint(__uint_as_float(sv[q][c + 3]) * ks.w);
-                            }
-                    }
-                    // a pair of weights as PV's operand
-                    auto operand = [&](float e0, float e1, int key) -> uint32_t {
-                        if (!FP8) return pack_bf16(e0, e1);
-                        const float2 vs = *reinterpret_cast<const float2*>(scales + (key >> 4) * 32 + 16 + (key & 15));
-                        const __half2 h = __floats2half2_rn(e0 * vs.x, e1 * vs.y);
-                        return *reinterpret_cast<const uint32_t*>(&h);
+                        for (int c = 0; c < 32; c += 4) {
+                            const float4 ks = *reinterpret_cast<const float4*>(scales + (q * 2 + (c >> 4)) * 32 + (c & 15));
+                            float a0, a1, a2, a3;
+                            unpack2(mul2(pack2(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), pack2(ks.x, ks.y)), a0, a1);
+                            unpack2(mul2(pack2(__uint_as_float(sv[c + 2]), __uint_as_float(sv[c + 3])), pack2(ks.z, ks.w)), a2, a3);
+                            sv[c] = __float_as_uint(a0), sv[c + 1] = __float_as_uint(a1), sv[c + 2] = __float_as_uint(a2), sv[c + 3] = __float_as_uint(a3);
+                        }
                     };
                     bool done = false;
                     if (!masked && k > 0) {
                         // Nearly every step leaves the running maximum as it is: weights and maximum at once, and again where one lies above.
+                        // (The second half's scores come under the first's exponentials.)
+                        uint32_t sa[32], sb[32], packed[32];
+                        tmem_ld32(s_addr, sa);
+                        tmem_wait_ld();
+                        tmem_ld32(s_addr + 32, sb);
                         const float m_sub = m == -INFINITY ? 0.f : m;
                         const uint64_t nm2 = pack2(-m_sub, -m_sub);
                         uint64_t ls0 = 0ull, ls1 = 0ull;
                         float mx0 = -INFINITY, mx1 = -INFINITY;
-                        uint32_t packed[32];
-#pragma unroll
-                        for (int q = 0; q < 2; ++q)
+                        auto weights = [&](uint32_t (&sv)[32], int q) {
+                            scaled(sv, q);
 #pragma unroll
                             for (int c = 0; c < 32; c += 2) {
+                                const float s0 = __uint_as_float(sv[c]), s1 = __uint_as_float(sv[c + 1]);
                                 float e0, e1;
-                                unpack2(fma2(pack2(__uint_as_float(sv[q][c]), __uint_as_float(sv[q][c + 1])), sc2, nm2), e0, e1);
+                                unpack2(fma2(pack2(s0, s1), sc2, nm2), e0, e1);
                                 e0 = fast_exp2(e0), e1 = fast_exp2(e1);
                                 if (c & 2) {
-                                    mx1 = max3(mx1, __uint_as_float(sv[q][c]), __uint_as_float(sv[q][c + 1]));
+                                    mx1 = max3(mx1, s0, s1);
                                     ls1 = add2(ls1, pack2(e0, e1));
                                 } else {
-                                    mx0 = max3(mx0, __uint_as_float(sv[q][c]), __uint_as_float(sv[q][c + 1]));
+                                    mx0 = max3(mx0, s0, s1);
                                     ls0 = add2(ls0, pack2(e0, e1));
                                 }
-                                packed[q * 16 + (c >> 1)] = operand(e0, e1, q * 32 + c);
+                                packed[q * 16 + (c >> 1)] = FP8 ? pack_f16(e0, e1) : pack_bf16(e0, e1);
                             }
+                        };
+                        weights(sa, 0);
+                        tmem_wait_ld();
+                        weights(sb, 1);
                         if (!__any_sync(0xffffffffu, fmaxf(mx0, mx1) * row_scale > m + kRescaleThreshold)) {
                             tmem_st32(s_addr, packed);
                             float a0, a1, a2, a3;
                             unpack2(ls0, a0, a1);
                             unpack2(ls1, a2, a3);
-                            const float sum = (a0 + a2) + (a1 + a3);
-                            lu += sum;
-                            l += sum;
+                            l += (a0 + a2) + (a1 + a3);
                             done = true;
                         }
                     }
                     if (!done) {
+                    uint32_t sv[2][32];
+                    tmem_ld32(s_addr, sv[0]);
+                    tmem_ld32(s_addr + 32, sv[1]);
+                    tmem_wait_ld();
+                    scaled(sv[0], 0);
+                    scaled(sv[1], 1);
                     if (masked) {
 #pragma unroll
-                        for (int q = 0; q < 2; ++q)
+                        for (int q = 0; q < 2; ++q) {
+                            const uint32_t vis = valid ? mask_bits(mask_row, mask0, mask1, key0 + 32 * q - it.prior, it.nodes) : 0u;
 #pragma unroll
                             for (int c = 0; c < 32; ++c)
-                                if (!(vis[q] >> c & 1u)) sv[q][c] = 0xff800000u;
+                                if (!(vis >> c & 1u)) sv[q][c] = 0xff800000u;
+                        }
                     }
                     float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
 #pragma unroll
@@ -452,13 +489,11 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                         tmem_wait_st();
                     }
                     l *= alpha;
-                    lu *= alpha;
                     m = m_new;
                     const float m_sub = m == -INFINITY ? 0.f : m;
                     const uint64_t nm2 = pack2(-m_sub, -m_sub);
                     // (masked scores are -inf, and their weights exp2(-inf) = 0)
                     uint64_t ls0 = 0ull, ls1 = 0ull;
-                    float l0 = 0.f, l1 = 0.f;
                     uint32_t packed[32];
 #pragma unroll
                     for (int q = 0; q < 2; ++q)
@@ -469,22 +504,13 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                             e0 = fast_exp2(e0), e1 = fast_exp2(e1);
                             if (c & 2) ls1 = add2(ls1, pack2(e0, e1));
                             else ls0 = add2(ls0, pack2(e0, e1));
-                            uint32_t w = operand(e0, e1, q * 32 + c);
-                            if (FP8 && masked) w &= (vis[q] >> c & 1u ? 0xffffu : 0u) | (vis[q] >> c & 2u ? 0xffff0000u : 0u);  // (what lies behind the end has any scale)
-                            packed[q * 16 + (c >> 1)] = w;
+                            packed[q * 16 + (c >> 1)] = FP8 ? pack_f16(e0, e1) : pack_bf16(e0, e1);
                         }
                     tmem_st32(s_addr, packed);
-                    if (masked && !FP8) {
-                        // (rows of few keys: the sum of the weights that PV multiplies keeps the output an exact mix of V rows)
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) l0 += bf16_lo(packed[c]), l1 += bf16_hi(packed[c]);
-                    }
                     float a0, a1, a2, a3;
                     unpack2(ls0, a0, a1);
                     unpack2(ls1, a2, a3);
-                    const float sum = (a0 + a2) + (a1 + a3);
-                    lu += sum;
-                    l += masked && !FP8 ? l0 + l1 : sum;
+                    l += (a0 + a2) + (a1 + a3);
                     }
                     tmem_wait_st();
                 }
@@ -505,12 +531,13 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
             int col0 = 0, col1 = D;
             uint32_t o0 = tmem + lane_addr + kColO + x * D, o1 = o0;
             if (n_x == 1) {
-                exchange[x * kRows + t] = make_float2(m, lu);
-                rounding[x * kRows + t] = __float2half_rn(lu > 0.f ? (l - lu) / lu : 0.f);
+                exchange[x * kRows + t] = make_float2(m, l);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bars + C::ex_full);
             }
             more = iter.next(ahead);  // (under the last PV)
+            if (more) keep(n_piece + 1, ahead);
+            if (FP8) it = kept_piece(n_piece);
             const uint32_t last = 8 * ((steps - 1) & 1), last_par = ((steps - 1) >> 1) & 1;
             ok = wait_all(bars + C::pv_done + 16 * x + last, last_par, s_abort);
             if (!ok) break;
@@ -521,16 +548,13 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                 if (ok) ok = wait_all(bars + C::pv_done + 16 * (x ^ 1) + last, last_par, s_abort);
                 if (!ok) break;
                 const float2 a = exchange[t], b = exchange[kRows + t];
-                const float ra = 1.f + __half2float(rounding[t]), rb = 1.f + __half2float(rounding[kRows + t]);
                 ++n_ex;
                 must_wait_free = true;
                 m = fmaxf(a.x, b.x);
                 const float m_sub = m == -INFINITY ? 0.f : m;
                 w0 = fast_exp2(a.x - m_sub);
                 w1 = fast_exp2(b.x - m_sub);
-                const float lu0 = a.y * w0, lu1 = b.y * w1;
-                lu = lu0 + lu1;
-                l = lu0 * ra + lu1 * rb;
+                l = a.y * w0 + b.y * w1;
                 o0 = tmem + lane_addr + kColO;
                 o1 = o0 + D;
                 col0 = x * (D / 2);
@@ -560,6 +584,10 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                         for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(fmaf(__uint_as_float(v[c]), w0, __uint_as_float(u[c]) * w1));
                     } else {
                         tmem_wait_ld();
+                    }
+                    if (FP8) {
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(2.f * __uint_as_float(v[c]));  // (V was halved)
                     }
                     if (flags && valid) {
                         // tree tokens whose V row was taken out of the products: their weight times that row
@@ -602,8 +630,8 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                     }
                 }
                 if (valid && col0 == 0) {
-                    if (!whole) p.part_ml[slot_row] = make_float4(m, l, lu, 0.f);
-                    else if (p.lse) p.lse[token * p.Hq + head] = lu > 0.f ? (m + log2f(lu)) * 0.6931471805599453f : lu == 0.f ? -INFINITY : lu;
+                    if (!whole) p.part_ml[slot_row] = make_float2(m, l);
+                    else if (p.lse) p.lse[token * p.Hq + head] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : l == 0.f ? -INFINITY : l;
                 }
             }
             tc_fence_before();
@@ -615,6 +643,7 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
             }
             q_tiles += n_x;
             tiles += n_tiles;
+            ++n_piece;
         }
     } else {
         if (warp == kLoadWarp) {
@@ -658,12 +687,13 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                     const uint32_t par = kv ? (n / C::kRaw) & 1 : at.par, dst = sbase + (kv ? C::kOffRaw + n % C::kRaw * C::kCodeBytes : at.at);
                     if (!wait_all(bars + free_, par ^ 1, s_abort)) return false;
                     if (elect_one()) {
-                        mbar_expect_tx(bars + land, C::kCodeBytes + (kv ? 0 : C::kScaleBytes));
+                        const uint32_t scales = sbase + (kv ? C::kOffRawScale + n % C::kRaw * C::kScaleBytes : C::kOffScale + n % C::kScaleTiles * C::kScaleBytes);
+                        mbar_expect_tx(bars + land, C::kCodeBytes + C::kScaleBytes);
                         s_armed[kv ? C::kSlots + 2 + n % C::kRaw : n % C::kSlots] = (int)par;
 #pragma unroll
                         for (int k = 0; k < 8; k += 4) {
                             gather4_at(dst + k * kPage * D, &pool_map, kv * (kPage * D / 8), r[k], r[k + 1], r[k + 2], r[k + 3], bars + land, policy);
-                            if (!kv) gather4_at(sbase + C::kOffScale + n % C::kScaleTiles * C::kScaleBytes + k * 128, &scale_map, 0, r[k], r[k + 1], r[k + 2], r[k + 3], bars + land, policy);
+                            gather4_at(scales + k * 128, &scale_map, 0, r[k], r[k + 1], r[k + 2], r[k + 3], bars + land, policy);
                         }
                     }
                 } else {
@@ -690,25 +720,26 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
             int page = -2, kv_head = 0;
             bool tree = false;
             fetch(page, kv_head, tree);
-            if (have) {
-                int row = pool_row(page, kv_head);
-                bool tree_v = tree;
-                fetch(page, kv_head, tree);
-                ok = load(row, 0, 0, false);
-                for (uint32_t n = 0; ok; ++n) {  // K of tile n + 1, V of tile n
-                    const int row_v = row;
-                    const bool more = have, raw = tree_v;
-                    if (more) {
-                        row = pool_row(page, kv_head);
-                        tree_v = tree;
-                        fetch(page, kv_head, tree);
-                        ok = load(row, n + 1, 0, false);
-                        if (!ok) break;
+            // K of tile n, then V of the one before
+            int row_k = -8, row_v = -8;
+            bool tree_v = false, more = have;
+            for (uint32_t n = 0; ok && (more || n > 0); ++n) {
+                for (int kv = 0; kv < 2 && ok; ++kv) {
+                    if (kv == 0) {
+                        row_v = row_k;
+                        if (!more) continue;
+                        row_k = pool_row(page, kv_head);
+                    } else if (n == 0) {
+                        continue;
                     }
-                    ok = load(row_v, n, 1, raw);
+                    const bool raw = kv && tree_v;
+                    ok = load(kv ? row_v : row_k, n - kv, kv, raw);
                     if (raw) ++n_raw;
-                    if (!more) break;
                 }
+                if (!more) break;
+                tree_v = tree;
+                fetch(page, kv_head, tree);
+                more = have;
             }
         } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
             // ================================================================
@@ -752,7 +783,7 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                     if (v_steps == k_steps) {
                         ok = wait_all(bars + ks.full, ks.par, s_abort);
                     } else {
-                        const int which = either(bars + ks.full, ks.par, bars + C::p_ready + 16 * x + 8 * vb, (v_steps >> 1) & 1);
+                        const int which = either(20, bars + ks.full, ks.par, bars + C::p_ready + 16 * x + 8 * vb, (v_steps >> 1) & 1);
                         ok = which != 0;
                         do_qk = which == 1;
                     }
@@ -821,11 +852,103 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                 ++sv;
                 ++v_steps;
             }
+        } else if (FP8 && warp == kQWarp) {
+            // ================================================================
+            // Q tiles, and each into two E4M3 numbers an element in its place.  Eight lanes have a row, 16 elements each.
+            // ================================================================
+            const int u = lane & 7;
+            uint32_t n = 0, n_split = 0, pending = 0;
+            bool ok = true;
+            auto split = [&](uint32_t qb) {
+                        char* const tile = smem + C::kOffQ + qb * C::kTileBytes;
+        #pragma unroll 1
+                        for (int i = 0; i < kRows / 4; ++i) {
+                            const int row = 4 * i + (lane >> 3);
+                            const char* const src = tile + (u >> 2) * C::kHalfBytes + row * 128;
+                            const uint4 a = *reinterpret_cast<const uint4*>(src + (((2 * u) ^ row) & 7) * 16), b = *reinterpret_cast<const uint4*>(src + (((2 * u + 1) ^ row) & 7) * 16);
+                            const uint32_t raw[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                            float x[16], top = 0.f;
+                            bool finite = true;
+        #pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                x[2 * k] = bf16_lo(raw[k]), x[2 * k + 1] = bf16_hi(raw[k]);
+                                top = fmaxf(top, fmaxf(fabsf(x[2 * k]), fabsf(x[2 * k + 1])));
+                            }
+                            finite = !any_not_finite(a) && !any_not_finite(b);
+        #pragma unroll
+                            for (int o = 4; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                            finite = (__ballot_sync(0xffffffffu, !finite) >> (lane & 24) & 0xffu) == 0;
+                            // 2^e with the row's largest times it in (224, 448]
+                            const int exponent = (int)(__float_as_uint(top) >> 23) - 127;  // (of a bf16 subnormal: -127)
+                            const bool high = (__float_as_uint(top) & 0x7fffffu) > 0x600000u;
+                            const int e = min(8 - exponent - (high ? 1 : 0), 120);
+                            const float up = __uint_as_float((uint32_t)(127 + e) << 23);
+                            uint32_t hi[4], lo[4];
+        #pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                float y[4], rest[4];
+                                uint32_t code = 0;
+        #pragma unroll
+                                for (int h = 0; h < 2; ++h) {
+                                    y[2 * h] = x[4 * k + 2 * h] * up, y[2 * h + 1] = x[4 * k + 2 * h + 1] * up;
+                                    uint16_t two;
+                                    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(y[2 * h + 1]), "f"(y[2 * h]));
+                                    code |= (uint32_t)two << (16 * h);
+                                    uint32_t back;
+                                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(back) : "h"(two));
+                                    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&back));
+                                    rest[2 * h] = y[2 * h] - f.x, rest[2 * h + 1] = y[2 * h + 1] - f.y;
+                                }
+                                hi[k] = code;
+                                uint16_t r0, r1;
+                                asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r0) : "f"(rest[1]), "f"(rest[0]));
+                                asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r1) : "f"(rest[3]), "f"(rest[2]));
+                                lo[k] = (uint32_t)r0 | (uint32_t)r1 << 16;
+                            }
+                            __syncwarp();  // (the row's other lanes have read what is overwritten)
+                            char* const dst = tile + row * 128 + (((u ^ row) & 7) << 4);
+                            *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                            *reinterpret_cast<uint4*>(dst + C::kHalfBytes) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                            if (u == 0) *reinterpret_cast<float*>(smem + C::kOffQScale + (qb * kRows + row) * 4) = finite ? __uint_as_float((uint32_t)(127 - e) << 23) : __uint_as_float(0x7fffffffu);
+                            __syncwarp();
+                        }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bars + C::q_ready + 8 * qb);
+            };
+            // (a tile is asked for before the one before it is split)
+            auto finish = [&]() {
+                if (pending == 0) return;
+                ok = wait_all(bars + C::q_full + 8 * (n_split & 1), (n_split >> 1) & 1, s_abort);
+                if (ok) split(n_split & 1);
+                ++n_split;
+                --pending;
+            };
+            while (ok && iter.next(it)) {
+                for (int x = 0; x < it.n_x(p.G) && ok; ++x, ++n) {
+                    if (!complete(bars + C::q_empty + 8 * (n & 1), ((n >> 1) & 1) ^ 1)) {
+                        finish();  // (what it waits for may need that tile)
+                        if (ok) ok = wait_all(bars + C::q_empty + 8 * (n & 1), ((n >> 1) & 1) ^ 1, s_abort);
+                        if (!ok) break;
+                    }
+                    if (elect_one()) {
+                        mbar_expect_tx(bars + C::q_full + 8 * (n & 1), C::kTileBytes);
+                        s_armed[C::kSlots + (n & 1)] = (int)((n >> 1) & 1);
+#pragma unroll
+                        for (int h = 0; h < C::kHalves; ++h)
+                            tma_load_3d(sbase + C::kOffQ + (n & 1) * C::kTileBytes + h * C::kHalfBytes, &q_map, h * 64, it.head * p.G, it.q_tok + x * tile_tok, bars + C::q_full + 8 * (n & 1));
+                    }
+                    __syncwarp();
+                    finish();
+                    ++pending;
+                }
+            }
+            if (ok) finish();
         } else if (warp == kQWarp) {
             // ================================================================
             // Q tiles: rows (token, head of the group) in token-major order, a box of [128 / G tokens][G heads][64 elements] per half; and V
             // rows that no product may read.  (Their tiles land on barriers of their own, and this warp's arrival takes the place of the
-            // copy's on the slot's; FP8: warps 12-15.)  An item's Q may have to wait for the end of the one before, and that for its V: whichever
+            // copy's on the slot's.)  An item's Q may have to wait for the end of the one before, and that for its V: whichever
             // can go on.
             // ================================================================
             PieceIter<Rows> iter_v = iter;
@@ -833,7 +956,7 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
             uint32_t n = 0, v_tile = 0, n_raw = 0;
             int x = 0, n_x = 0;        // q tile of the item, of that many
             int j = 0;                 // key tile of the item whose V comes next
-            bool ok = true, have_q = iter.next(it), have_v = !FP8 && iter_v.next(iv);
+            bool ok = true, have_q = iter.next(it), have_v = iter_v.next(iv);
             n_x = it.n_x(p.G);
             auto begin_v = [&]() {     // to the item's first tile with tree tokens, past those that have none
                 while (have_v) {
@@ -846,7 +969,7 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
             begin_v();
             while (ok && (have_q || have_v)) {
                 const uint32_t bq = bars + C::q_empty + 8 * (n & 1), pq = ((n >> 1) & 1) ^ 1, bv = bars + C::raw + 8 * (n_raw % C::kRaw), pv = n_raw / C::kRaw & 1;
-                const int which = have_q && have_v ? either(bq, pq, bv, pv) : wait_all(have_q ? bq : bv, have_q ? pq : pv, s_abort) ? (have_q ? 1 : 2) : 0;
+                const int which = have_q && have_v ? either(200, bq, pq, bv, pv) : wait_all(have_q ? bq : bv, have_q ? pq : pv, s_abort) ? (have_q ? 1 : 2) : 0;
                 ok = which != 0;
                 if (which == 1) {
                     if (elect_one()) {
@@ -900,108 +1023,57 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
 
     if constexpr (FP8) if (warp >= kConvertWarp) {
         // ====================================================================
-        // FP8: q tiles into two E4M3 numbers an element, in their place, and V's codes into f16; 32 rows of each a warp, whichever tile
-        // can be worked on.  Eight lanes have a row, 16 elements each.
+        // FP8: V's codes into f16; 32 rows of a tile a warp.  Eight lanes have a row, 16 elements each.
         // ====================================================================
         const int w = warp - kConvertWarp, u = lane & 7;
-        PieceIter<Rows> iter_v = iter;
-        Piece iv;
-        uint32_t n_q = 0, n_v = 0;
-        int left_q = 0, j = 0;
-        bool ok = true, have_q = iter.next(it), have_v = iter_v.next(iv);
-        left_q = it.n_x(p.G);
-        j = iv.tile0;
-        while (ok && (have_q || have_v)) {
-            const uint32_t qb = n_q & 1, vb = n_v & 1, rb = n_v % C::kRaw;
-            const int which = poll([&]() {
-                if (have_q && complete(bars + C::q_full + 8 * qb, (n_q >> 1) & 1)) return 1;
-                return have_v && complete(bars + C::raw + 8 * rb, (n_v / C::kRaw) & 1) && complete(bars + C::conv_empty + 8 * vb, ((n_v >> 1) & 1) ^ 1) ? 2 : 0;
-            });
-            ok = which != 0;
-            if (which == 1) {
-                char* const tile = smem + C::kOffQ + qb * C::kTileBytes;
-#pragma unroll 2
-                for (int i = 0; i < 8; ++i) {
-                    const int row = 32 * w + 4 * i + (lane >> 3);
-                    const char* const src = tile + (u >> 2) * C::kHalfBytes + row * 128;
-                    const uint4 a = *reinterpret_cast<const uint4*>(src + (((2 * u) ^ row) & 7) * 16), b = *reinterpret_cast<const uint4*>(src + (((2 * u + 1) ^ row) & 7) * 16);
-                    const uint32_t raw[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-                    float x[16], top = 0.f;
-                    bool finite = true;
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        x[2 * k] = bf16_lo(raw[k]), x[2 * k + 1] = bf16_hi(raw[k]);
-                        top = fmaxf(top, fmaxf(fabsf(x[2 * k]), fabsf(x[2 * k + 1])));
-                    }
-                    finite = !any_not_finite(a) && !any_not_finite(b);
-#pragma unroll
-                    for (int o = 4; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                    finite = (__ballot_sync(0xffffffffu, !finite) >> (lane & 24) & 0xffu) == 0;
-                    // 2^e with the row's largest times it in (224, 448]
-                    const int exponent = (int)(__float_as_uint(top) >> 23) - 127;  // (of a bf16 subnormal: -127)
-                    const bool high = (__float_as_uint(top) & 0x7fffffu) > 0x600000u;
-                    const int e = min(8 - exponent - (high ? 1 : 0), 120);
-                    const float up = __uint_as_float((uint32_t)(127 + e) << 23);
-                    uint32_t hi[4], lo[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        float y[4], rest[4];
-                        uint32_t code = 0;
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            y[2 * h] = x[4 * k + 2 * h] * up, y[2 * h + 1] = x[4 * k + 2 * h + 1] * up;
-                            uint16_t two;
-                            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(y[2 * h + 1]), "f"(y[2 * h]));
-                            code |= (uint32_t)two << (16 * h);
-                            uint32_t back;
-                            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(back) : "h"(two));
-                            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&back));
-                            rest[2 * h] = y[2 * h] - f.x, rest[2 * h + 1] = y[2 * h + 1] - f.y;
-                        }
-                        hi[k] = code;
-                        uint16_t r0, r1;
-                        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r0) : "f"(rest[1]), "f"(rest[0]));
-                        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r1) : "f"(rest[3]), "f"(rest[2]));
-                        lo[k] = (uint32_t)r0 | (uint32_t)r1 << 16;
-                    }
-                    __syncwarp();  // (the row's other lanes have read what is overwritten)
-                    char* const dst = tile + row * 128 + (((u ^ row) & 7) << 4);
-                    *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                    *reinterpret_cast<uint4*>(dst + C::kHalfBytes) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                    if (u == 0) *reinterpret_cast<float*>(smem + C::kOffQScale + (qb * kRows + row) * 4) = finite ? __uint_as_float((uint32_t)(127 - e) << 23) : __uint_as_float(0x7fffffffu);
-                    __syncwarp();
-                }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bars + C::q_ready + 8 * qb);
-                ++n_q;
-                if (--left_q == 0) {
-                    have_q = iter.next(it);
-                    left_q = it.n_x(p.G);
-                }
-            } else if (which == 2) {
-                const bool tree = j >= iv.tree_tile();
+        uint32_t n_v = 0;
+        bool ok = true;
+        while (ok && iter.next(it)) {
+            for (int j = it.tile0; j < it.tile1; ++j, ++n_v) {
+                const uint32_t vb = n_v & 1, rb = n_v % C::kRaw;
+                ok = wait_all(bars + C::raw + 8 * rb, (n_v / C::kRaw) & 1, s_abort);
+                if (ok) ok = wait_all(bars + C::conv_empty + 8 * vb, ((n_v >> 1) & 1) ^ 1, s_abort);
+                if (!ok) break;
+                const bool tree = j >= it.tree_tile();
                 const char* const src = smem + C::kOffRaw + rb * C::kCodeBytes;
                 char* const dst = smem + C::kOffConv + vb * C::kTileBytes + (u >> 2) * C::kHalfBytes;
                 uint32_t flags = 0;
-#pragma unroll 2
+                // (rolled, a row ahead of its loads: this code shares the instruction cache with four other roles')
+                const char* from = src + (32 * w + (lane >> 3)) * 128;
+                const float* scale_at = reinterpret_cast<const float*>(smem + C::kOffRawScale + rb * C::kScaleBytes) + 2 * w * 32 + 16 + (lane >> 3);
+                uint4 next = *reinterpret_cast<const uint4*>(from + (((u ^ (lane >> 3)) & 7) << 4));
+                float next_scale = *scale_at;
+#pragma unroll 1
                 for (int i = 0; i < 8; ++i) {
                     const int row = 32 * w + 4 * i + (lane >> 3), key = j * kTileKeys + row;
-                    uint4 code = *reinterpret_cast<const uint4*>(src + row * 128 + (((u ^ row) & 7) << 4));
+                    uint4 code = next;
+                    const float vs = next_scale;
+                    if (i < 7) {
+                        next = *reinterpret_cast<const uint4*>(from + (i + 1) * 512 + (((u ^ (row + 4)) & 7) << 4));
+                        next_scale = scale_at[(i + 1 >> 2) * 32 + (i + 1 & 3) * 4];
+                    }
+                    bool gone = false;
                     if (tree) {
                         auto nan = [](uint32_t c) { return (((c & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0; };
-                        const bool odd = key >= iv.prior && key < iv.kv_len && (nan(code.x) || nan(code.y) || nan(code.z) || nan(code.w));
+                        const bool odd = key >= it.prior && key < it.kv_len && (nan(code.x) || nan(code.y) || nan(code.z) || nan(code.w) || !isfinite(vs));
                         const uint32_t any = __ballot_sync(0xffffffffu, odd);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) flags |= (any >> (8 * k) & 0xffu ? 1u : 0u) << (4 * i + k);
-                        if (key >= iv.kv_len || (any >> (lane & 24) & 0xffu)) code = make_uint4(0, 0, 0, 0);
+                        gone = key >= it.kv_len || (any >> (lane & 24) & 0xffu);
+                        if (gone) code = make_uint4(0, 0, 0, 0);
                     }
+                    const __half2 by = __float2half2_rn(gone ? 0.f : 0.5f * vs);
                     const uint32_t c[4] = {code.x, code.y, code.z, code.w};
                     uint32_t y[8];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * k]) : "h"((uint16_t)c[k]));
                         asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[2 * k + 1]) : "h"((uint16_t)(c[k] >> 16)));
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&y[k]), by);
+                        y[k] = *reinterpret_cast<const uint32_t*>(&v);
                     }
                     // (the halves' lanes begin at different units: no bank conflicts)
                     const bool swap = u & 4;
@@ -1015,11 +1087,6 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                 if (lane == 0) {
                     mbar_arrive(bars + C::conv_full + 8 * vb);
                     mbar_arrive(bars + C::raw_empty + 8 * rb);
-                }
-                ++n_v;
-                if (++j == iv.tile1) {
-                    have_v = iter_v.next(iv);
-                    j = iv.tile0;
                 }
             }
         }
@@ -1088,15 +1155,15 @@ __global__ void __launch_bounds__(kMergeThreads) tree_merge_kernel(const __grid_
     int n_seg = 2;
     while (share_begin(p, c + n_seg - 1) < end) ++n_seg;
     auto place = [&](int s) { return (int64_t)(2 * (c - 1 + s) + (s == 0 ? 1 : 0)) * kGroupRows; };
-    float M[kMergeRows], l[kMergeRows], lu[kMergeRows], acc[kMergeRows][V];
+    float M[kMergeRows], l[kMergeRows], acc[kMergeRows][V];
 #pragma unroll
     for (int k = 0; k < kMergeRows; ++k) {
-        M[k] = -INFINITY, l[k] = lu[k] = 0.f;
+        M[k] = -INFINITY, l[k] = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) acc[k][v] = 0.f;
     }
     for (int s = 0; s < n_seg; ++s) {
-        float4 ml[kMergeRows];
+        float2 ml[kMergeRows];
         float x[kMergeRows][V];
 #pragma unroll
         for (int k = 0; k < kMergeRows; ++k) {
@@ -1112,7 +1179,6 @@ __global__ void __launch_bounds__(kMergeThreads) tree_merge_kernel(const __grid_
             const float a = fast_exp2(M[k] - base), b = fast_exp2(ml[k].x - base);
             M[k] = top;
             l[k] = fmaf(l[k], a, ml[k].y * b);
-            lu[k] = fmaf(lu[k], a, ml[k].z * b);
 #pragma unroll
             for (int v = 0; v < V; ++v) acc[k][v] = fmaf(acc[k][v], a, x[k][v] * b);
         }
@@ -1126,13 +1192,13 @@ __global__ void __launch_bounds__(kMergeThreads) tree_merge_kernel(const __grid_
         uint32_t* const dst = reinterpret_cast<uint32_t*>(p.out + at * D + lane * V);
 #pragma unroll
         for (int v = 0; v < V; v += 2) dst[v / 2] = pack_bf16(acc[k][v] * inv, acc[k][v + 1] * inv);
-        if (p.lse && lane == 0) p.lse[at] = lu[k] > 0.f ? (M[k] + log2f(lu[k])) * 0.6931471805599453f : lu[k] == 0.f ? -INFINITY : lu[k];
+        if (p.lse && lane == 0) p.lse[at] = l[k] > 0.f ? (M[k] + log2f(l[k])) * 0.6931471805599453f : l[k] == 0.f ? -INFINITY : l[k];
     }
 }
 
 constexpr int kSms = 148;  // of the device that the library is built for: CTAs, and places in the workspace
 
-size_t workspace_bytes(const ps_shape& s) { return 2 * (size_t)kSms * kGroupRows * (s.head_dim * sizeof(float) + sizeof(float4)); }
+size_t workspace_bytes(const ps_shape& s) { return 2 * (size_t)kSms * kGroupRows * (s.head_dim * sizeof(float) + sizeof(float2)); }
 
 struct TreeCall {
     const KvPool* pool;
@@ -1195,8 +1261,8 @@ ps_status launch_rows(const TreeCall& a) {
     p.pool = a.pool->base;
     p.out = (__nv_bfloat16*)a.out;
     p.lse = a.lse;
-    p.part_ml = (float4*)a.ws;
-    p.part_o = (float*)(a.ws + 2 * (size_t)kSms * kGroupRows * sizeof(float4));
+    p.part_ml = (float2*)a.ws;
+    p.part_o = (float*)(a.ws + 2 * (size_t)kSms * kGroupRows * sizeof(float2));
     p.flag = a.pool->flag_dev;
     p.num_pages = a.pool->num_pages;
     p.wait_limit_ns = (uint32_t)a.pool->wait_limit_ns;
