@@ -9,7 +9,7 @@
 // share a kv head.
 //
 // Work: an item is one (request, kv head, group of up to 256 rows).  Its keys are tiles of 128, and all items' tiles, with
-// kItemUnits more an item for its start and end, make one line that is cut into equal shares, a CTA each, wherever the cuts fall
+// some more an item for its start and end, make one line that is cut into equal shares, a CTA each, wherever the cuts fall
 // (stream-K).  So one request on a long context, or a ragged batch, fills all SMs, and a CTA has at most two pieces of an item:
 // partial rows go to fixed places of the workspace and tree_merge_kernel joins them in the order of their keys.  The shares
 // follow from the batch's lengths, which travel as kernel parameters: there is no work list to upload and nothing to
@@ -46,12 +46,14 @@ constexpr int kLoadWarp = 8, kMmaWarp = 9, kQWarp = 11, kConvertWarp = 12;  // (
 constexpr int kTileKeys = 128, kRows = 128;
 constexpr int kGroupRows = 2 * kRows;      // rows of an item
 constexpr int kMaxNodes = 256;
-constexpr int kItemUnits = 1;              // what an item's start and end cost, in key tiles
 constexpr float kRescaleThreshold = 8.f;   // log2 units
 
 template <int D, bool FP8>
 struct Cfg {
     static constexpr int kThreads = FP8 ? 512 : 384;         // (of three warps a scheduler each may have 168 registers)
+    // What an item's start and end cost, in key tiles.  Measured with 1 / 3 / 4 / 6 / 9: 32 trees of 11-32 nodes on 500-4000 tokens, 128 dimensions 76.0 /
+    // 71.7 / 71.7 / 71.2 / 73.4 us; 24 of 20-61 on 300-5000, 64 dimensions 48.6 / 44.0 / 44.7 / 46.0 / 47.5; FP8, 64 of 7-32 on 500-4000 183 / 167 / 160 / 152 / 155.
+    static constexpr int kItemUnits = FP8 ? 7 : D == 128 ? 5 : 3;
     static constexpr int kHalves = D / 64;
     static constexpr int kHalfBytes = kTileKeys * 128;
     static constexpr int kTileBytes = kHalves * kHalfBytes;  // a tile of Q, K or V in 16 bits
@@ -124,7 +126,7 @@ struct TreeParams {
     int* flag;
     int64_t num_pages;
     uint32_t wait_limit_ns;
-    int32_t max_pages, mask_words, n, Hq, Hkv, G, units, share, longer;  // a share's units; the first `longer` shares have one more
+    int32_t max_pages, mask_words, n, Hq, Hkv, G, item_units, share, longer;  // a share's units; the first `longer` shares have one more
 };
 
 // pieces of items in a CTA's share of the line
@@ -142,20 +144,20 @@ __device__ __forceinline__ int share_begin(const TreeParams& p, int c) { return 
 template <class Rows>
 struct PieceIter {
     const Rows& rows;
-    int G, Hkv, left, r, head, group, w0;  // units left of the share; where it goes on: request, kv head, group, units into the item
+    int G, Hkv, extra, left, r, head, group, w0;  // units of an item beside its tiles; units left of the share; where it goes on: request, kv head, group, units into the item
     __device__ __forceinline__ int tiles() const { return (rows.prior[r] + rows.q_start[r + 1] - rows.q_start[r] + kTileKeys - 1) / kTileKeys; }
     __device__ __forceinline__ int groups(int nodes) const {
         const int shift = 31 - __clz(kGroupRows / G);  // (G is a power of two)
         return (nodes + (1 << shift) - 1) >> shift;
     }
-    __device__ __forceinline__ PieceIter(const Rows& rows_, int n, int G_, int Hkv_, int u, int end) : rows(rows_), G(G_), Hkv(Hkv_), left(end - u) {
+    __device__ __forceinline__ PieceIter(const Rows& rows_, int n, int G_, int Hkv_, int extra_, int u, int end) : rows(rows_), G(G_), Hkv(Hkv_), extra(extra_), left(end - u) {
         int lo = 0, hi = n - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (rows.unit_start[mid] <= u) lo = mid; else hi = mid - 1;
         }
         r = lo;
-        const int per = tiles() + kItemUnits, o = u - rows.unit_start[r], item = o / per, gr = groups(rows.q_start[r + 1] - rows.q_start[r]);
+        const int per = tiles() + extra, o = u - rows.unit_start[r], item = o / per, gr = groups(rows.q_start[r + 1] - rows.q_start[r]);
         w0 = o - item * per;
         head = item / gr;
         group = item - head * gr;
@@ -169,9 +171,9 @@ struct PieceIter {
             x.kv_len = x.prior + x.nodes;
             x.tiles = tiles();
             x.head = head;
-            x.tile0 = max(0, w0 - kItemUnits);
-            x.tile1 = max(0, min(x.tiles + kItemUnits, w0 + left) - kItemUnits);
-            left -= x.tiles + kItemUnits - w0;
+            x.tile0 = max(0, w0 - extra);
+            x.tile1 = max(0, min(x.tiles + extra, w0 + left) - extra);
+            left -= x.tiles + extra - w0;
             w0 = 0;
             const int tok0 = group * (kGroupRows / G);
             x.n_tok = min(kGroupRows / G, x.nodes - tok0);
@@ -304,14 +306,14 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + C::kOffBar + C::tmem_slot);
     auto wait_all = [](uint32_t bar, uint32_t parity, volatile int* abort_flag) { return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag)); };
 
-    // f() until it is not 0, polled for at most about the wait limit; 0 then.  (Between polls the warp sleeps: every question takes
-    // its turn in the queue that the other warps' shared-memory accesses go through.)
+    // f() until it is not 0, polled for at most about the wait limit; 0 then.  (Sleep between polls only where the answer is not urgent: a sleep of
+    // 20 ns puts the MMA warps some 700 cycles behind.)
     auto poll = [&](uint32_t sleep_ns, auto f) -> int {
         uint32_t t0 = 0;
         for (uint32_t i = 1;; ++i) {
             const int got = f();
             if (got) return got;
-            __nanosleep(sleep_ns);
+            if (sleep_ns) __nanosleep(sleep_ns);
             const uint32_t limit_ns = (uint32_t)s_abort[1];
             if ((i & 15) == 0 || limit_ns == 0) {
                 const uint32_t now = global_timer_lo() | 1u;
@@ -329,7 +331,7 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
     };
 
     constexpr uint32_t kColO = 256;
-    PieceIter<Rows> iter(rows, p.n, p.G, p.Hkv, share_begin(p, blockIdx.x), share_begin(p, blockIdx.x + 1));
+    PieceIter<Rows> iter(rows, p.n, p.G, p.Hkv, C::kItemUnits, share_begin(p, blockIdx.x), share_begin(p, blockIdx.x + 1));
     Piece it;
     const int tile_tok = kRows / p.G, g_shift = 31 - __clz(p.G);
 
@@ -783,7 +785,7 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                     if (v_steps == k_steps) {
                         ok = wait_all(bars + ks.full, ks.par, s_abort);
                     } else {
-                        const int which = either(20, bars + ks.full, ks.par, bars + C::p_ready + 16 * x + 8 * vb, (v_steps >> 1) & 1);
+                        const int which = either(0, bars + ks.full, ks.par, bars + C::p_ready + 16 * x + 8 * vb, (v_steps >> 1) & 1);
                         ok = which != 0;
                         do_qk = which == 1;
                     }
@@ -1141,11 +1143,11 @@ __global__ void __launch_bounds__(kMergeThreads) tree_merge_kernel(const __grid_
         r = lo;
     }
     const int prior = rows.prior[r], q_tok = rows.q_start[r], nodes = rows.q_start[r + 1] - q_tok;
-    const int tiles = (prior + nodes + kTileKeys - 1) / kTileKeys, per = tiles + kItemUnits;
+    const int tiles = (prior + nodes + kTileKeys - 1) / kTileKeys, per = tiles + p.item_units;
     const int item = (border - rows.unit_start[r]) / per, begin = rows.unit_start[r] + item * per, end = begin + per;
     pdl_wait();
     // (a border at an item's begin cuts nothing, nor does one before its first tile; and the item is the first border's inside it)
-    const int first_tile = begin + kItemUnits;
+    const int first_tile = begin + p.item_units;
     if (border <= first_tile || share_begin(p, c - 1) > first_tile) return;
     const int group_tok = kGroupRows / p.G, groups = (nodes + group_tok - 1) / group_tok;
     const int head = item / groups, tok0 = (item - head * groups) * group_tok, n_rows = min(group_tok, nodes - tok0) * p.G;
@@ -1231,7 +1233,7 @@ ps_status launch_rows(const TreeCall& a) {
         tokens += a.n_nodes[r];
         const int groups = (a.n_nodes[r] + group_tok - 1) / group_tok;
         wide = wide || groups > 1;
-        units += (int64_t)Hkv * groups * (((int64_t)a.prior[r] + a.n_nodes[r] + kTileKeys - 1) / kTileKeys + kItemUnits);
+        units += (int64_t)Hkv * groups * (((int64_t)a.prior[r] + a.n_nodes[r] + kTileKeys - 1) / kTileKeys + Cfg<D, FP8>::kItemUnits);
         if (units > 0x3fffffff) return fail(PS_ERR_INVALID, "too many keys in one batch");
     }
     rows.q_start[a.n] = tokens;
@@ -1266,8 +1268,8 @@ ps_status launch_rows(const TreeCall& a) {
     p.flag = a.pool->flag_dev;
     p.num_pages = a.pool->num_pages;
     p.wait_limit_ns = (uint32_t)a.pool->wait_limit_ns;
-    p.max_pages = a.max_pages, p.mask_words = a.mask_words, p.n = a.n, p.Hq = Hq, p.Hkv = Hkv, p.G = G, p.units = (int32_t)units;
-    const int grid = (int)(units / 2 < kSms ? units / 2 : kSms);  // (an item has at least two units: no share is empty)
+    p.max_pages = a.max_pages, p.mask_words = a.mask_words, p.n = a.n, p.Hq = Hq, p.Hkv = Hkv, p.G = G, p.item_units = Cfg<D, FP8>::kItemUnits;
+    const int grid = (int)(units / 2 < kSms ? units / 2 : kSms);
     p.share = (int32_t)units / grid, p.longer = (int32_t)units % grid;
     st = launch_kernel(tree_kernel<D, FP8, Rows>, grid, Cfg<D, FP8>::kThreads, Cfg<D, FP8>::kSmemBytes, a.stream, 1, true, p, q_map, pool_map, scale_map, rows);
     if (st != PS_OK || grid == 1) return st;
