@@ -392,14 +392,15 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                     // FP8: times the keys' scales, 16 of K and 16 of V a page
                     const float* const scales = reinterpret_cast<const float*>(smem + C::kOffScale + (tiles + tile) % C::kScaleTiles * C::kScaleBytes) + half * 128;
                     auto scaled = [&](uint32_t (&sv)[32], int q) {
-                        if (!FP8) return;
+                        if constexpr (FP8) {
 #pragma unroll
-                        for (int c = 0; c < 32; c += 4) {
-                            const float4 ks = *reinterpret_cast<const float4*>(scales + (q * 2 + (c >> 4)) * 32 + (c & 15));
-                            float a0, a1, a2, a3;
-                            unpack2(mul2(pack2(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), pack2(ks.x, ks.y)), a0, a1);
-                            unpack2(mul2(pack2(__uint_as_float(sv[c + 2]), __uint_as_float(sv[c + 3])), pack2(ks.z, ks.w)), a2, a3);
-                            sv[c] = __float_as_uint(a0), sv[c + 1] = __float_as_uint(a1), sv[c + 2] = __float_as_uint(a2), sv[c + 3] = __float_as_uint(a3);
+                            for (int c = 0; c < 32; c += 4) {
+                                const float4 ks = *reinterpret_cast<const float4*>(scales + (q * 2 + (c >> 4)) * 32 + (c & 15));
+                                float a0, a1, a2, a3;
+                                unpack2(mul2(pack2(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), pack2(ks.x, ks.y)), a0, a1);
+                                unpack2(mul2(pack2(__uint_as_float(sv[c + 2]), __uint_as_float(sv[c + 3])), pack2(ks.z, ks.w)), a2, a3);
+                                sv[c] = __float_as_uint(a0), sv[c + 1] = __float_as_uint(a1), sv[c + 2] = __float_as_uint(a2), sv[c + 3] = __float_as_uint(a3);
+                            }
                         }
                     };
                     bool done = false;
@@ -444,75 +445,76 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                             done = true;
                         }
                     }
-                    if (!done) {
-                    uint32_t sv[2][32];
-                    tmem_ld32(s_addr, sv[0]);
-                    tmem_ld32(s_addr + 32, sv[1]);
-                    tmem_wait_ld();
-                    scaled(sv[0], 0);
-                    scaled(sv[1], 1);
-                    if (masked) {
+                    // (said to be rare, so that the compiler lays this code out of the loop's way: the instruction cache holds little more than the loop)
+                    if (__builtin_expect(!done, 0)) {
+                        uint32_t sv[2][32];
+                        tmem_ld32(s_addr, sv[0]);
+                        tmem_ld32(s_addr + 32, sv[1]);
+                        tmem_wait_ld();
+                        scaled(sv[0], 0);
+                        scaled(sv[1], 1);
+                        if (masked) {
 #pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            const uint32_t vis = valid ? mask_bits(mask_row, mask0, mask1, key0 + 32 * q - it.prior, it.nodes) : 0u;
+                            for (int q = 0; q < 2; ++q) {
+                                const uint32_t vis = valid ? mask_bits(mask_row, mask0, mask1, key0 + 32 * q - it.prior, it.nodes) : 0u;
 #pragma unroll
-                            for (int c = 0; c < 32; ++c)
-                                if (!(vis >> c & 1u)) sv[q][c] = 0xff800000u;
+                                for (int c = 0; c < 32; ++c)
+                                    if (!(vis >> c & 1u)) sv[q][c] = 0xff800000u;
+                            }
                         }
-                    }
-                    float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
+                        float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
 #pragma unroll
-                    for (int q = 0; q < 2; ++q)
+                        for (int q = 0; q < 2; ++q)
 #pragma unroll
-                        for (int c = 0; c < 32; c += 8) {
-                            mx0 = max3(mx0, __uint_as_float(sv[q][c]), __uint_as_float(sv[q][c + 1]));
-                            mx1 = max3(mx1, __uint_as_float(sv[q][c + 2]), __uint_as_float(sv[q][c + 3]));
-                            mx2 = max3(mx2, __uint_as_float(sv[q][c + 4]), __uint_as_float(sv[q][c + 5]));
-                            mx3 = max3(mx3, __uint_as_float(sv[q][c + 6]), __uint_as_float(sv[q][c + 7]));
-                        }
-                    const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * row_scale;
-                    const float m_new = mx > m + kRescaleThreshold ? mx : m;  // also the first finite maximum
-                    const float alpha = m_new == m ? 1.f : fast_exp2(m - m_new);
-                    if (k > 0 && __any_sync(0xffffffffu, m_new != m)) {
-                        // the accumulator as of the step before (what came before that was complete when these scores were)
-                        ok = wait_all(bars + C::pv_done + 16 * x + 8 * (buf ^ 1), ((steps - 1) >> 1) & 1, s_abort);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint32_t o_addr = tmem + lane_addr + kColO + x * D;
+                            for (int c = 0; c < 32; c += 8) {
+                                mx0 = max3(mx0, __uint_as_float(sv[q][c]), __uint_as_float(sv[q][c + 1]));
+                                mx1 = max3(mx1, __uint_as_float(sv[q][c + 2]), __uint_as_float(sv[q][c + 3]));
+                                mx2 = max3(mx2, __uint_as_float(sv[q][c + 4]), __uint_as_float(sv[q][c + 5]));
+                                mx3 = max3(mx3, __uint_as_float(sv[q][c + 6]), __uint_as_float(sv[q][c + 7]));
+                            }
+                        const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * row_scale;
+                        const float m_new = mx > m + kRescaleThreshold ? mx : m;  // also the first finite maximum
+                        const float alpha = m_new == m ? 1.f : fast_exp2(m - m_new);
+                        if (k > 0 && __any_sync(0xffffffffu, m_new != m)) {
+                            // the accumulator as of the step before (what came before that was complete when these scores were)
+                            ok = wait_all(bars + C::pv_done + 16 * x + 8 * (buf ^ 1), ((steps - 1) >> 1) & 1, s_abort);
+                            if (!ok) break;
+                            tc_fence_after();
+                            const uint32_t o_addr = tmem + lane_addr + kColO + x * D;
 #pragma unroll 1
-                        for (int c0 = 0; c0 < D; c0 += 32) {
-                            uint32_t v[32];
-                            tmem_ld32(o_addr + c0, v);
-                            tmem_wait_ld();
+                            for (int c0 = 0; c0 < D; c0 += 32) {
+                                uint32_t v[32];
+                                tmem_ld32(o_addr + c0, v);
+                                tmem_wait_ld();
 #pragma unroll
-                            for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(__uint_as_float(v[c]) * alpha);
-                            tmem_st32(o_addr + c0, v);
+                                for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(__uint_as_float(v[c]) * alpha);
+                                tmem_st32(o_addr + c0, v);
+                            }
+                            tmem_wait_st();
                         }
-                        tmem_wait_st();
-                    }
-                    l *= alpha;
-                    m = m_new;
-                    const float m_sub = m == -INFINITY ? 0.f : m;
-                    const uint64_t nm2 = pack2(-m_sub, -m_sub);
-                    // (masked scores are -inf, and their weights exp2(-inf) = 0)
-                    uint64_t ls0 = 0ull, ls1 = 0ull;
-                    uint32_t packed[32];
+                        l *= alpha;
+                        m = m_new;
+                        const float m_sub = m == -INFINITY ? 0.f : m;
+                        const uint64_t nm2 = pack2(-m_sub, -m_sub);
+                        // (masked scores are -inf, and their weights exp2(-inf) = 0)
+                        uint64_t ls0 = 0ull, ls1 = 0ull;
+                        uint32_t packed[32];
 #pragma unroll
-                    for (int q = 0; q < 2; ++q)
+                        for (int q = 0; q < 2; ++q)
 #pragma unroll
-                        for (int c = 0; c < 32; c += 2) {
-                            float e0, e1;
-                            unpack2(fma2(pack2(__uint_as_float(sv[q][c]), __uint_as_float(sv[q][c + 1])), sc2, nm2), e0, e1);
-                            e0 = fast_exp2(e0), e1 = fast_exp2(e1);
-                            if (c & 2) ls1 = add2(ls1, pack2(e0, e1));
-                            else ls0 = add2(ls0, pack2(e0, e1));
-                            packed[q * 16 + (c >> 1)] = FP8 ? pack_f16(e0, e1) : pack_bf16(e0, e1);
-                        }
-                    tmem_st32(s_addr, packed);
-                    float a0, a1, a2, a3;
-                    unpack2(ls0, a0, a1);
-                    unpack2(ls1, a2, a3);
-                    l += (a0 + a2) + (a1 + a3);
+                            for (int c = 0; c < 32; c += 2) {
+                                float e0, e1;
+                                unpack2(fma2(pack2(__uint_as_float(sv[q][c]), __uint_as_float(sv[q][c + 1])), sc2, nm2), e0, e1);
+                                e0 = fast_exp2(e0), e1 = fast_exp2(e1);
+                                if (c & 2) ls1 = add2(ls1, pack2(e0, e1));
+                                else ls0 = add2(ls0, pack2(e0, e1));
+                                packed[q * 16 + (c >> 1)] = FP8 ? pack_f16(e0, e1) : pack_bf16(e0, e1);
+                            }
+                        tmem_st32(s_addr, packed);
+                        float a0, a1, a2, a3;
+                        unpack2(ls0, a0, a1);
+                        unpack2(ls1, a2, a3);
+                        l += (a0 + a2) + (a1 + a3);
                     }
                     tmem_wait_st();
                 }
@@ -591,7 +593,7 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
 #pragma unroll
                         for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(2.f * __uint_as_float(v[c]));  // (V was halved)
                     }
-                    if (flags && valid) {
+                    if (__builtin_expect(flags != 0 && valid, 0)) {
                         // tree tokens whose V row was taken out of the products: their weight times that row
 #pragma unroll 1
                         for (int w = 4 * max(it.tile0, it.tree_tile()); w < 4 * it.tile1; ++w) {  // 32 keys
