@@ -180,7 +180,8 @@ typedef struct {
  * aligned.  Asynchronous on `stream`.  Errors: PS_ERR_INVALID, PS_ERR_UNSUPPORTED
  * (rot_dim), PS_ERR_CUDA; a token whose page lies outside the pool or whose
  * position lies outside the table is skipped, q_out's row included, and
- * reported by ps_kv_status.
+ * reported by ps_kv_status, as is a wait inside the kernel that ran out (some
+ * tokens are then missing).
  */
 ps_status ps_kv_write_rope(ps_kv *kv, const ps_rope *args, const int32_t *block_table_dev, int32_t max_pages, const int32_t *prior_host,
                            const int32_t *q_len_host, int32_t n, void *stream);
@@ -208,7 +209,7 @@ ps_status ps_attn_tree(const ps_kv *kv, const void *q_dev, const int32_t *block_
                        int32_t mask_words, const int32_t *prior_host, const int32_t *n_nodes_host, int32_t n, void *out_dev,
                        float *lse_out_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
 
-/* Bound of every wait inside ps_attn_tree's kernels, as ps_plan_set_wait_limit's. */
+/* Bound of every wait inside the kernels of ps_attn_tree and ps_kv_write_rope, as ps_plan_set_wait_limit's. */
 ps_status ps_kv_set_wait_limit(ps_kv *kv, int64_t limit_ns);
 
 /*

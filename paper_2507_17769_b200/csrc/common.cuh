@@ -117,7 +117,7 @@ struct KvPool {
     int32_t* meta_dev;   // q_start[n+1], prior[n] for ps_kv_write
     int32_t meta_cap;    // ints
     int32_t* flag_dev;   // kStatus* bits of the kernels that have no plan
-    int64_t wait_limit_ns;  // of the tree kernel's waits
+    int64_t wait_limit_ns;  // of the waits in kernels that have no plan
 };
 
 const KvPool& pool_of(const ps_kv* kv);

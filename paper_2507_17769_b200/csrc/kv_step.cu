@@ -3,6 +3,7 @@
 #include <type_traits>
 
 #include "kv_rows.cuh"
+#include "tcgen05.cuh"
 
 namespace ps {
 
@@ -15,12 +16,21 @@ namespace {
 //     (a, b) -> (a cos - b sin, b cos + a sin)     (pairs of the first rot_dim elements)
 //
 // q goes to its output, k and v to their pages.  Everything between the load and the store is fp32: a key is rounded once, to bf16
-// or, in an FP8 cache, to its code.  A CTA has one token: D / 8 lanes hold a head, 16 bytes each, so the norm is a sum over 8 or
-// 16 lanes, a rotated pair's other half (half-split pairs) comes by shuffle from the lane rot_dim / 16 away, and a lane's angles are the
-// same for every head of the token and are loaded once.
+// or, in an FP8 cache, to its code.  D / 8 lanes hold a head, 16 bytes each, so the norm is a sum over 8 or 16 lanes, a rotated pair's
+// other half (half-split pairs) comes by shuffle from the lane rot_dim / 16 away, and a lane's angles and norm weights are the same for
+// every head of their kind and are loaded once a token.  Bound by memory and, nearly as much, by instructions: some 60 a warp and pair of
+// heads with two elements an instruction.  Measured: 6722 tokens of 32 + 8 + 8 heads of 128, 166 MB, in 36 us (4.6 TB/s; 50 us with a CTA a
+// token); 2560 tokens of 64 + 8 + 8 into an FP8 cache, 99 MB, in 29 us.
 // ---------------------------------------------------------------------------
 constexpr int kRopeThreads = 256;
-constexpr int kRopeAhead = 3;  // heads of a lane whose loads are under way together
+constexpr int kRopeAhead = 3;     // few tokens: heads of a lane whose loads are under way together
+// Many tokens: four stages a CTA and two CTAs an SM.  (32 + 8 + 8 heads, bf16: 3000 tokens take 18.8 us with four stages and two teams of
+// four warps, 17.8 with eight stages and four teams of two, but 6722 tokens 36 us against 39; one team of eight warps 23.1, a warp a token 28.)
+constexpr int kRopeStages = 4, kRopeTeams = 2, kRopeTeamWarps = kRopeThreads / 32 / kRopeTeams;
+constexpr int kRopeRingBytes = 108 * 1024, kRopeRingCtas = 2 * 148;
+// Up to here a CTA a token is faster: all of them run at once and none waits for a stage.  (The same heads, a CTA a token and in
+// stretches: 64 tokens 3.4 and 5.9 us, 256 4.1 and 6.6, 400 7.3 and 6.0, 900 12.5 and 8.8; FP8 256 4.7 and 8.1, 400 8.3 and 7.0.)
+constexpr int kRopeFew = 2 * 148;
 
 struct RopeParams {
     char* pool;
@@ -35,136 +45,298 @@ struct RopeParams {
     const int32_t* block_table;
     int* flag;
     float eps;
-    int32_t rot_dim, interleaved, max_pages, n, Hq, Hkv;
+    uint32_t wait_limit_ns;
+    int32_t rot_dim, interleaved, max_pages, n, Hq, Hkv, tokens, stage_bytes;
 };
 
-__device__ __forceinline__ void widen8(const uint4& x, float (&y)[8]) {
-    y[0] = bf16_lo(x.x), y[1] = bf16_hi(x.x), y[2] = bf16_lo(x.y), y[3] = bf16_hi(x.y);
-    y[4] = bf16_lo(x.z), y[5] = bf16_hi(x.z), y[6] = bf16_lo(x.w), y[7] = bf16_hi(x.w);
-}
-__device__ __forceinline__ uint4 narrow8(const float (&y)[8]) {
-    return make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
-}
+__device__ __forceinline__ uint64_t widened(uint32_t two) { return pack2(bf16_lo(two), bf16_hi(two)); }
 
+// A lane's part of a head: y = x a + x' b over its 8 elements, x' the other elements of their pairs, a and b the angles times the norm's weights.
+template <int D, bool FP8>
+struct RopeLane {
+    static constexpr int L = D / 8;  // lanes of a head
+    const RopeParams& p;
+    int l, e0, other;  // the lane within its head, its first element, the lane of its pairs' other elements
+    bool turns;
+    uint4 wq, wq_other, wk, wk_other;
+    struct Kind {
+        uint64_t a[4], b[4];  // of pairs of elements
+    };
+
+    __device__ __forceinline__ explicit RopeLane(const RopeParams& params) : p(params) {
+        const int half = p.rot_dim >> 1;
+        l = threadIdx.x % L, e0 = 8 * l;
+        turns = e0 < p.rot_dim;
+        other = !turns || p.interleaved ? l : e0 < half ? l + half / 8 : l - half / 8;
+        wq = wq_other = wk = wk_other = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);  // ones
+        if (p.q_weight) wq = __ldg(reinterpret_cast<const uint4*>(p.q_weight + e0)), wq_other = __ldg(reinterpret_cast<const uint4*>(p.q_weight + 8 * other));
+        if (p.k_weight) wk = __ldg(reinterpret_cast<const uint4*>(p.k_weight + e0)), wk_other = __ldg(reinterpret_cast<const uint4*>(p.k_weight + 8 * other));
+        if (p.interleaved) wq_other = swapped(wq), wk_other = swapped(wk);
+    }
+    static __device__ __forceinline__ uint4 swapped(const uint4& x) {  // the pairs themselves, turned round
+        return make_uint4(__byte_perm(x.x, 0, 0x1032), __byte_perm(x.y, 0, 0x1032), __byte_perm(x.z, 0, 0x1032), __byte_perm(x.w, 0, 0x1032));
+    }
+    // cosines and, with the sign of the other element's part, sines of the lane's elements, from a row of the table
+    __device__ __forceinline__ Kind angles(const float* row) const {
+        Kind f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f.a[i] = pack2(1.f, 1.f), f.b[i] = 0ull;
+        if (!turns) return f;
+        const int half = p.rot_dim >> 1;
+        if (p.interleaved) {
+            const float4 c = *reinterpret_cast<const float4*>(row + e0 / 2), s = *reinterpret_cast<const float4*>(row + half + e0 / 2);
+            f.a[0] = pack2(c.x, c.x), f.a[1] = pack2(c.y, c.y), f.a[2] = pack2(c.z, c.z), f.a[3] = pack2(c.w, c.w);
+            f.b[0] = pack2(-s.x, s.x), f.b[1] = pack2(-s.y, s.y), f.b[2] = pack2(-s.z, s.z), f.b[3] = pack2(-s.w, s.w);
+        } else {
+            const float* const at = row + (e0 < half ? e0 : e0 - half);
+            const float sign = e0 < half ? -1.f : 1.f;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float4 c = reinterpret_cast<const float4*>(at)[i], s = reinterpret_cast<const float4*>(at + half)[i];
+                f.a[2 * i] = pack2(c.x, c.y), f.a[2 * i + 1] = pack2(c.z, c.w);
+                f.b[2 * i] = pack2(sign * s.x, sign * s.y), f.b[2 * i + 1] = pack2(sign * s.z, sign * s.w);
+            }
+        }
+        return f;
+    }
+    __device__ __forceinline__ static Kind weighted(const Kind& f, const uint4& w4, const uint4& wo4) {
+        const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w}, wo[4] = {wo4.x, wo4.y, wo4.z, wo4.w};
+        Kind g;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) g.a[i] = mul2(f.a[i], widened(w[i])), g.b[i] = mul2(f.b[i], widened(wo[i]));
+        return g;
+    }
+    // 1 / root mean square of the head, by all lanes of a warp
+    __device__ __forceinline__ float inverse_rms(const uint64_t (&y)[4]) const {
+        uint64_t ss2 = 0ull;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ss2 = fma2(y[i], y[i], ss2);
+        float s0, s1;
+        unpack2(ss2, s0, s1);
+        float ss = s0 + s1;
+#pragma unroll
+        for (int o = L / 2; o >= 1; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        return rsqrtf(ss * (1.f / D) + p.eps);
+    }
+    // y: the lane's elements, x_other: the others of their pairs
+    __device__ __forceinline__ void turn(uint64_t (&y)[4], const uint4& x_other, const Kind& f, bool normed, float rstd) const {
+        const uint32_t xo[4] = {x_other.x, x_other.y, x_other.z, x_other.w};
+        const uint64_t by = pack2(rstd, rstd);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint64_t z = widened(xo[i]);
+            if (normed) y[i] = mul2(y[i], by), z = mul2(z, by);  // (first, so that no product with a weight overflows)
+            y[i] = mul2(y[i], f.a[i]);
+            if (turns) y[i] = fma2(z, f.b[i], y[i]);
+        }
+    }
+    __device__ __forceinline__ void store16(char* dst, const uint64_t (&y)[4]) const {
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) unpack2(y[i], f[2 * i], f[2 * i + 1]);
+        *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+    }
+    // The lane's part of a key (which = 0) or value (1) of kv head g to its page; by all lanes of a warp, some of which store nothing.
+    __device__ __forceinline__ void store_kv(const uint64_t (&y)[4], int g, int which, int64_t page, int slot, bool yes) const {
+        if (!FP8) {
+            if (yes) store16(p.pool + (page * p.Hkv + g) * (int64_t)page_head_bytes(D) + which * block_bytes(D) + unit_offset(slot, e0), y);
+            return;
+        }
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) unpack2(y[i], f[2 * i], f[2 * i + 1]);
+        float amax = fmaxf(fabsf(f[0]), fabsf(f[1]));
+#pragma unroll
+        for (int i = 2; i < 8; i += 2) amax = max3(amax, fabsf(f[i]), fabsf(f[i + 1]));
+#pragma unroll
+        for (int o = L / 2; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+        if (!yes) return;
+        const float scale = fp8_scale(amax);
+        char* const blk = p.pool + (page * p.Hkv + g) * (int64_t)fp8_page_head_bytes(D);
+        *reinterpret_cast<uint2*>(blk + which * (kPage * D) + slot * D + (((l >> 1) ^ (slot & 7)) << 4) + 8 * (l & 1)) =
+            make_uint2(quantise4(f[0], f[1], f[2], f[3], scale), quantise4(f[4], f[5], f[6], f[7], scale));
+        if (l == 0) reinterpret_cast<float*>(blk + 2 * kPage * D)[which * kPage + slot] = scale;
+    }
+};
+
+// Few tokens: a CTA has one.  Bound by latency: the lookup of the request, then the page and the heads together, then the angles.
 template <int D, bool FP8, class Rows>
 __global__ void __launch_bounds__(kRopeThreads) write_rope_kernel(const RopeParams p, const __grid_constant__ Rows rows) {
-    constexpr int L = D / 8;                      // lanes of a head
-    constexpr int kGroups = kRopeThreads / L;
+    constexpr int L = D / 8, kGroups = kRopeThreads / L;
     pdl_trigger();
-    const int t = blockIdx.x, lane = threadIdx.x & 31, l = threadIdx.x % L, group = threadIdx.x / L;
+    const int t = blockIdx.x, group = threadIdx.x / L;
     const int r = request_of(rows, p.n, t);
     const int pos = rows.prior(r) + (t - rows.q_start(r)), slot = pos % kPage;
+    const int n_vec = p.Hq + 2 * p.Hkv;
     pdl_wait();
     const int64_t page = p.block_table[(int64_t)r * p.max_pages + pos / kPage];
     const int64_t angle = p.positions ? p.positions[t] : pos;
-    if (page < 0 || page >= p.num_pages || (p.rot_dim > 0 && (angle < 0 || angle >= p.n_positions))) {
-        if (threadIdx.x == 0) atomicOr(p.flag, kStatusBounds);
-        return;
-    }
-    const int half = p.rot_dim >> 1, e0 = 8 * l;
-    const bool turns = e0 < p.rot_dim;
-    // lane of the same head that holds the other elements of this lane's pairs, and the sign of their part
-    const int other = !turns || p.interleaved ? l : e0 < half ? l + half / 8 : l - half / 8;
-    const int other_lane = lane - l + other;
-    float cosv[8], sinv[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) cosv[i] = 1.f, sinv[i] = 0.f;
-    if (turns) {
-        const float* const row = p.cos_sin + angle * p.rot_dim + (p.interleaved ? e0 / 2 : e0 < half ? e0 : e0 - half);
-#pragma unroll
-        for (int i = 0; i < 8; i += 4) {
-            if (!p.interleaved || i == 0) {
-                const float4 c = *reinterpret_cast<const float4*>(row + i), s = *reinterpret_cast<const float4*>(row + half + i);
-                cosv[i] = c.x, cosv[i + 1] = c.y, cosv[i + 2] = c.z, cosv[i + 3] = c.w;
-                sinv[i] = s.x, sinv[i + 1] = s.y, sinv[i + 2] = s.z, sinv[i + 3] = s.w;
-            }
-        }
-        if (!p.interleaved && e0 < half) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sinv[i] = -sinv[i];
-        }
-    }
-    const int n_vec = p.Hq + 2 * p.Hkv;
-    for (int v0 = group; v0 - group < n_vec; v0 += kGroups * kRopeAhead) {  // (the warp's lanes stay together: they shuffle)
-        uint4 raw[kRopeAhead];
+    const RopeLane<D, FP8> mine(p);
+    const int other_lane = (threadIdx.x & 31) - mine.l + mine.other;
+    const __nv_bfloat16 *const q_row = p.q + (int64_t)t * p.q_stride + mine.e0, *const k_row = p.k + (int64_t)t * p.k_stride + mine.e0,
+                              *const v_row = p.v + (int64_t)t * p.v_stride + mine.e0;
+    uint4 raw[kRopeAhead];
+    auto load = [&](int v0) {
 #pragma unroll
         for (int a = 0; a < kRopeAhead; ++a) {
             const int vec = v0 + a * kGroups;
             raw[a] = make_uint4(0, 0, 0, 0);
-            if (vec < n_vec) {
-                const __nv_bfloat16* src = vec < p.Hq          ? p.q + (int64_t)t * p.q_stride + vec * D
-                                           : vec < p.Hq + p.Hkv ? p.k + (int64_t)t * p.k_stride + (vec - p.Hq) * D
-                                                                : p.v + (int64_t)t * p.v_stride + (vec - p.Hq - p.Hkv) * D;
-                raw[a] = *reinterpret_cast<const uint4*>(src + e0);
-            }
+            if (vec < n_vec)
+                raw[a] = *reinterpret_cast<const uint4*>(vec < p.Hq ? q_row + vec * D : vec < p.Hq + p.Hkv ? k_row + (vec - p.Hq) * D : v_row + (vec - p.Hq - p.Hkv) * D);
         }
+    };
+    load(group);
+    if (page < 0 || page >= p.num_pages || (p.rot_dim > 0 && (angle < 0 || angle >= p.n_positions))) {
+        if (threadIdx.x == 0) atomicOr(p.flag, kStatusBounds);
+        return;
+    }
+    const auto f = mine.angles(p.cos_sin + angle * p.rot_dim);
+#pragma unroll 1
+    for (int v0 = group; v0 - group < n_vec; v0 += kGroups * kRopeAhead) {  // (the same number of steps in every lane of a warp: they shuffle)
+        if (v0 != group) load(v0);
 #pragma unroll
         for (int a = 0; a < kRopeAhead; ++a) {
             const int vec = v0 + a * kGroups;
-            if (vec - group >= n_vec) break;  // (the same for the whole warp)
+            if (vec - group >= n_vec) continue;
             const bool is_q = vec < p.Hq, is_v = vec >= p.Hq + p.Hkv;
-            float x[8];
-            widen8(raw[a], x);
-            float ss = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-#pragma unroll
-            for (int o = L / 2; o >= 1; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-            uint4 raw_other;
-            raw_other.x = __shfl_sync(0xffffffffu, raw[a].x, other_lane);
-            raw_other.y = __shfl_sync(0xffffffffu, raw[a].y, other_lane);
-            raw_other.z = __shfl_sync(0xffffffffu, raw[a].z, other_lane);
-            raw_other.w = __shfl_sync(0xffffffffu, raw[a].w, other_lane);
-            float y[8];
-            widen8(raw_other, y);
-            const __nv_bfloat16* const weight = is_q ? p.q_weight : p.k_weight;
-            if (!is_v) {
-                if (weight) {
-                    const float rstd = rsqrtf(ss * (1.f / D) + p.eps);
-                    float w[8], wo[8];
-                    widen8(__ldg(reinterpret_cast<const uint4*>(weight + e0)), w);
-                    widen8(__ldg(reinterpret_cast<const uint4*>(weight + 8 * other)), wo);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] *= rstd * w[i], y[i] *= rstd * wo[i];
-                }
-                if (turns) {
-                    if (p.interleaved) {
-#pragma unroll
-                        for (int i = 0; i < 8; i += 2) {
-                            const float c = cosv[i >> 1], s = sinv[i >> 1], b = x[i + 1];
-                            x[i + 1] = fmaf(b, c, x[i] * s);
-                            x[i] = fmaf(x[i], c, -(b * s));
-                        }
+            const uint4 x = raw[a];
+            uint64_t y[4] = {widened(x.x), widened(x.y), widened(x.z), widened(x.w)};
+            if (!__all_sync(0xffffffffu, is_v)) {
+                const bool normed = is_q ? p.q_weight != nullptr : p.k_weight != nullptr;
+                const float rstd = mine.inverse_rms(y);
+                uint4 xo;
+                xo.x = __shfl_sync(0xffffffffu, x.x, other_lane), xo.y = __shfl_sync(0xffffffffu, x.y, other_lane);
+                xo.z = __shfl_sync(0xffffffffu, x.z, other_lane), xo.w = __shfl_sync(0xffffffffu, x.w, other_lane);
+                if (p.interleaved) xo = mine.swapped(x);
+                if (!is_v) mine.turn(y, xo, is_q ? mine.weighted(f, mine.wq, mine.wq_other) : mine.weighted(f, mine.wk, mine.wk_other), normed, rstd);
+            }
+            if (is_q) mine.store16(reinterpret_cast<char*>(p.q_out + ((int64_t)t * p.Hq + vec) * D + mine.e0), y);
+            if (!__all_sync(0xffffffffu, is_q)) mine.store_kv(y, vec - p.Hq - (is_v ? p.Hkv : 0), is_v, page, slot, !is_q && vec < n_vec);
+        }
+    }
+}
+
+// Many tokens: a CTA has a stretch of them.  Its last warp looks the tokens up, 32 at a time, and sends a token's three rows and its angles to
+// shared memory by bulk copies; the others work in two teams, a token each, so that what a token needs once (angles times weights) is
+// worked out in four warps, and a team's next token is under way meanwhile.  A stage is always the same team's: both sides of its
+// barriers see every phase.
+template <int D, bool FP8, class Rows>
+__global__ void __launch_bounds__(kRopeThreads + 32, 2) write_rope_ring_kernel(const RopeParams p, const __grid_constant__ Rows rows) {
+    constexpr int L = D / 8, kWarps = kRopeThreads / 32;
+    extern __shared__ __align__(128) char smem[];
+    __shared__ uint64_t s_bar[2 * kRopeStages];  // full, empty
+    __shared__ int2 s_where[kRopeStages];        // page (-1: the token is passed over) and slot
+    __shared__ int s_abort[2];
+    pdl_trigger();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t full = smem_u32(s_bar), empty = full + 8 * kRopeStages;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kRopeStages; ++s) mbar_init(full + 8 * s, 1), mbar_init(empty + 8 * s, kRopeTeamWarps);
+        mbar_fence_init();
+        s_abort[0] = 0, s_abort[1] = (int)p.wait_limit_ns;
+    }
+    __syncthreads();
+    pdl_wait();
+    const int t0 = (int)((int64_t)p.tokens * blockIdx.x / gridDim.x), n = (int)((int64_t)p.tokens * (blockIdx.x + 1) / gridDim.x) - t0;
+    const uint32_t q_bytes = p.Hq * D * 2, kv_bytes = p.Hkv * D * 2, angle_bytes = p.rot_dim * 4;
+    if (warp == kWarps) {
+        const uint64_t policy = l2_policy_evict_first();
+        int stage = 0, issued = 0;
+        uint32_t par = 0;
+        bool ok = true;
+        for (int i0 = 0; ok && i0 < n; i0 += 32) {
+            const int m = min(32, n - i0), t = t0 + i0 + min(lane, m - 1);
+            const int r = request_of(rows, p.n, t);
+            const int pos = rows.prior(r) + (t - rows.q_start(r));
+            int page = p.block_table[(int64_t)r * p.max_pages + pos / kPage];
+            const int angle = p.positions ? p.positions[t] : pos;
+            if (page < 0 || page >= p.num_pages || (p.rot_dim > 0 && (angle < 0 || angle >= p.n_positions))) {
+                atomicOr(p.flag, kStatusBounds);
+                page = -1;
+            }
+            for (int i = 0; i < m; ++i) {
+                ok = __all_sync(0xffffffffu, wait_or_abort(empty + 8 * stage, par ^ 1, s_abort));
+                if (!ok) break;
+                const int page_i = __shfl_sync(0xffffffffu, page, i), slot_i = __shfl_sync(0xffffffffu, pos % kPage, i);
+                const int64_t angle_i = __shfl_sync(0xffffffffu, angle, i), t_i = t0 + i0 + i;
+                if (lane == 0) {
+                    s_where[stage] = make_int2(page_i, slot_i);
+                    const uint32_t bar = full + 8 * stage, dst = smem_u32(smem) + stage * p.stage_bytes;
+                    if (page_i < 0) {
+                        mbar_arrive(bar);
                     } else {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) x[i] = fmaf(x[i], cosv[i], y[i] * sinv[i]);
+                        mbar_expect_tx(bar, q_bytes + 2 * kv_bytes + angle_bytes);
+                        bulk_g2s_hint(dst, p.q + t_i * p.q_stride, q_bytes, bar, policy);
+                        bulk_g2s_hint(dst + q_bytes, p.k + t_i * p.k_stride, kv_bytes, bar, policy);
+                        bulk_g2s_hint(dst + q_bytes + kv_bytes, p.v + t_i * p.v_stride, kv_bytes, bar, policy);
+                        if (angle_bytes) bulk_g2s_hint(dst + q_bytes + 2 * kv_bytes, p.cos_sin + angle_i * p.rot_dim, angle_bytes, bar, policy);
                     }
                 }
+                __syncwarp();
+                ++issued;
+                if (++stage == kRopeStages) stage = 0, par ^= 1;
             }
-            float scale = 1.f;
-            if (FP8) {
-                float amax = 0.f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(x[i]));
-#pragma unroll
-                for (int o = L / 2; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-                scale = fp8_scale(amax);
+        }
+        __syncwarp();
+        // what is under way lands before the block ends (as it does by itself where no wait ran out)
+        for (int i = max(0, issued - kRopeStages); i < issued; ++i) mbar_wait(full + 8 * (i % kRopeStages), (i / kRopeStages) & 1, kDrainLimitNs);
+        if (!ok && lane == 0) atomicOr(p.flag, kStatusTimeout);
+    } else {
+        const RopeLane<D, FP8> mine(p);
+        constexpr int kHeads = 32 / L;  // of a warp
+        constexpr int kStep = kRopeTeamWarps * kHeads;
+        const int team = warp / kRopeTeamWarps, first = warp % kRopeTeamWarps * kHeads, sub = lane / L;
+        int stage = team;
+        uint32_t par = 0;
+        for (int i = team; i < n; i += kRopeTeams) {
+            if (!__all_sync(0xffffffffu, wait_or_abort(full + 8 * stage, par, s_abort))) {
+                if (lane == 0) atomicOr(p.flag, kStatusTimeout);
+                break;
             }
-            if (vec >= n_vec) continue;
-            if (is_q) {
-                *reinterpret_cast<uint4*>(p.q_out + ((int64_t)t * p.Hq + vec) * D + e0) = narrow8(x);
-            } else {
-                const int g = vec - p.Hq - (is_v ? p.Hkv : 0);
-                if (FP8) {
-                    char* const blk = p.pool + (page * p.Hkv + g) * (int64_t)fp8_page_head_bytes(D);
-                    *reinterpret_cast<uint2*>(blk + (is_v ? kPage * D : 0) + slot * D + (((l >> 1) ^ (slot & 7)) << 4) + 8 * (l & 1)) =
-                        make_uint2(quantise4(x[0], x[1], x[2], x[3], scale), quantise4(x[4], x[5], x[6], x[7], scale));
-                    if (l == 0) reinterpret_cast<float*>(blk + 2 * kPage * D)[(is_v ? kPage : 0) + slot] = scale;
-                } else {
-                    char* const blk = p.pool + (page * p.Hkv + g) * (int64_t)page_head_bytes(D) + (is_v ? block_bytes(D) : 0);
-                    *reinterpret_cast<uint4*>(blk + unit_offset(slot, e0)) = narrow8(x);
+            const int2 where = s_where[stage];
+            if (where.x >= 0) {
+                const char* const src = smem + stage * p.stage_bytes;
+                const float* const row = reinterpret_cast<const float*>(src + q_bytes + 2 * kv_bytes);
+                const char* const mine_at = src + 2 * mine.e0;
+                // a head's elements, normed and turned
+                auto worked = [&](uint64_t (&y)[4], const char* at, const auto& f, bool normed) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(at);
+                    y[0] = widened(x.x), y[1] = widened(x.y), y[2] = widened(x.z), y[3] = widened(x.w);
+                    const float rstd = normed ? mine.inverse_rms(y) : 1.f;
+                    mine.turn(y, p.interleaved ? mine.swapped(x) : *reinterpret_cast<const uint4*>(at + 16 * (mine.other - mine.l)), f, normed, rstd);
+                };
+                {
+                    const auto f = mine.weighted(mine.angles(row), mine.wq, mine.wq_other);
+                    const bool normed = p.q_weight != nullptr;
+                    char* const out = reinterpret_cast<char*>(p.q_out + (int64_t)(t0 + i) * p.Hq * D + mine.e0);
+#pragma unroll 2
+                    for (int h0 = first; h0 < p.Hq; h0 += kStep) {
+                        const int h = min(h0 + sub, p.Hq - 1);
+                        uint64_t y[4];
+                        worked(y, mine_at + h * (2 * D), f, normed);
+                        if (h == h0 + sub) mine.store16(out + h * (2 * D), y);
+                    }
+                }
+                const auto f = mine.weighted(mine.angles(row), mine.wk, mine.wk_other);
+                const bool normed = p.k_weight != nullptr;
+#pragma unroll 1
+                for (int g0 = first; g0 < p.Hkv; g0 += kStep) {
+                    const int g = min(g0 + sub, p.Hkv - 1);
+                    uint64_t y[4];
+                    worked(y, mine_at + q_bytes + g * (2 * D), f, normed);
+                    mine.store_kv(y, g, 0, where.x, where.y, g == g0 + sub);
+                }
+#pragma unroll 1
+                for (int g0 = first; g0 < p.Hkv; g0 += kStep) {
+                    const int g = min(g0 + sub, p.Hkv - 1);
+                    const uint4 x = *reinterpret_cast<const uint4*>(mine_at + q_bytes + kv_bytes + g * (2 * D));
+                    const uint64_t y[4] = {widened(x.x), widened(x.y), widened(x.z), widened(x.w)};
+                    mine.store_kv(y, g, 1, where.x, where.y, g == g0 + sub);
                 }
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(empty + 8 * stage);
+            if ((stage += kRopeTeams) >= kRopeStages) stage = team, par ^= 1;
         }
     }
 }
@@ -202,10 +374,11 @@ __global__ void __launch_bounds__(kAcceptThreads) accept_kernel(const AcceptPara
     const int nodes = rows.q_start(r + 1) - rows.q_start(r), prior = rows.prior(r);
     const int count = p.count[r];
     const int32_t* const index = p.index + (int64_t)r * p.index_stride;
+    int node = lane < p.index_stride ? index[lane] : 0;  // (under way with the count)
     bool good = count >= 0 && count <= nodes && count <= p.index_stride;
     if (good) {
         for (int i = lane; i < count; i += 32) {
-            const int at = index[i];
+            const int at = i == lane ? node : index[i];
             good = good && at >= i && at < nodes && (i == 0 || at > index[i - 1]);
         }
     }
@@ -215,44 +388,52 @@ __global__ void __launch_bounds__(kAcceptThreads) accept_kernel(const AcceptPara
     }
     const int32_t* const table = p.block_table + (int64_t)r * p.max_pages;
     const int64_t head_bytes = FP8 ? fp8_page_head_bytes(D) : page_head_bytes(D);
-    auto place = [&](int node) -> char* {  // of this lane's part of a token; null: no such page
-        const int pos = prior + node, slot = pos % kPage;
-        const int64_t page = table[pos / kPage];
-        if (page < 0 || page >= p.num_pages) return nullptr;
-        char* const blk = p.pool + (page * p.Hkv + g) * head_bytes;
+    char* const pool = p.pool + g * head_bytes;
+    auto part = [&](int32_t page, int slot) -> char* {  // this lane's part of a token
+        char* const blk = pool + (int64_t)page * p.Hkv * head_bytes;
         if (FP8) {
             if (lane >= 2 * kUnits) return blk + 2 * kPage * D + ((lane - 2 * kUnits) * kPage + slot) * 4;
             return blk + (lane / kUnits) * (kPage * D) + slot * D + (((lane % kUnits) ^ (slot & 7)) << 4);
         }
         return blk + (lane / kUnits) * block_bytes(D) + unit_offset(slot, 8 * (lane % kUnits));
     };
-    for (int i0 = 0; i0 < count; i0 += kAcceptAhead) {
-        uint4 x[kAcceptAhead];
-        char* dst[kAcceptAhead];
-#pragma unroll
-        for (int a = 0; a < kAcceptAhead; ++a) {
-            const int i = i0 + a;
-            dst[a] = nullptr;
-            if (i < count) {
-                const int at = index[i];
-                if (at == i) continue;  // it is there already
-                const char* const src = place(at);
-                dst[a] = place(i);
-                if (!src || !dst[a]) {
-                    if (lane == 0) atomicOr(p.flag, kStatusBounds);
-                    dst[a] = nullptr;
-                } else if (lane < 2 * kUnits) {
-                    x[a] = *reinterpret_cast<const uint4*>(src);
-                } else if (lane < kLanes) {
-                    x[a].x = *reinterpret_cast<const uint32_t*>(src);
-                }
+    for (int c0 = 0; c0 < count; c0 += 32) {
+        // lane a: where the path's token c0 + a is and where it goes
+        const int mine = c0 + lane;
+        if (c0 > 0 && mine < count) node = index[mine];
+        int32_t from = 0, to = 0;
+        bool moves = mine < count && node != mine;  // (else it is there already)
+        if (moves) {
+            from = table[(prior + node) / kPage], to = table[(prior + mine) / kPage];
+            if (from < 0 || from >= p.num_pages || to < 0 || to >= p.num_pages) {
+                atomicOr(p.flag, kStatusBounds);
+                moves = false;
             }
         }
+        const uint32_t moving = __ballot_sync(0xffffffffu, moves);
+        const int n = min(32, count - c0), from_slot = (prior + node) % kPage;
+        for (int i0 = 0; i0 < n; i0 += kAcceptAhead) {
+            uint4 x[kAcceptAhead];
+            int32_t to_page[kAcceptAhead];
 #pragma unroll
-        for (int a = 0; a < kAcceptAhead; ++a) {
-            if (!dst[a]) continue;
-            if (lane < 2 * kUnits) *reinterpret_cast<uint4*>(dst[a]) = x[a];
-            else if (lane < kLanes) *reinterpret_cast<uint32_t*>(dst[a]) = x[a].x;
+            for (int a = 0; a < kAcceptAhead; ++a) {
+                const int i = i0 + a;
+                const int32_t page = __shfl_sync(0xffffffffu, from, i);
+                const int slot = __shfl_sync(0xffffffffu, from_slot, i);
+                to_page[a] = __shfl_sync(0xffffffffu, to, i);
+                if (moving >> i & 1u) {
+                    const char* const src = part(page, slot);
+                    if (lane < 2 * kUnits) x[a] = *reinterpret_cast<const uint4*>(src);
+                    else if (lane < kLanes) x[a].x = *reinterpret_cast<const uint32_t*>(src);
+                }
+            }
+#pragma unroll
+            for (int a = 0; a < kAcceptAhead; ++a) {
+                if (!(moving >> (i0 + a) & 1u)) continue;
+                char* const dst = part(to_page[a], (prior + c0 + i0 + a) % kPage);
+                if (lane < 2 * kUnits) *reinterpret_cast<uint4*>(dst) = x[a];
+                else if (lane < kLanes) *reinterpret_cast<uint32_t*>(dst) = x[a].x;
+            }
         }
     }
 }
@@ -449,8 +630,24 @@ ps_status ps_kv_write_rope(ps_kv* kv, const ps_rope* a, const int32_t* block_tab
         p.eps = a->eps;
         p.rot_dim = a->rot_dim, p.interleaved = a->interleaved, p.max_pages = max_pages;
         p.n = m, p.Hq = Hq, p.Hkv = Hkv;
-        auto* const kernel = pool.shape.dtype == 1 ? write_rope_kernel<128, true, Rows> : d == 128 ? write_rope_kernel<128, false, Rows> : write_rope_kernel<64, false, Rows>;
-        return launch_kernel(kernel, tokens, kRopeThreads, 0, (cudaStream_t)stream, 1, true, p, rows);
+        p.wait_limit_ns = (uint32_t)pool.wait_limit_ns;
+        p.tokens = tokens;
+        p.stage_bytes = (Hq + 2 * Hkv) * d * 2 + a->rot_dim * 4;
+        const auto launch = [&](auto d_, auto fp8_) -> ps_status {
+            constexpr int D = decltype(d_)::value;
+            constexpr bool FP8 = decltype(fp8_)::value;
+            if (tokens <= kRopeFew || p.stage_bytes * kRopeStages > kRopeRingBytes) return launch_kernel(write_rope_kernel<D, FP8, Rows>, tokens, kRopeThreads, 0, (cudaStream_t)stream, 1, true, p, rows);
+            static PerDeviceOnce configured;
+            const ps_status st = once_per_device(configured, []() -> ps_status {
+                PS_CUDA_TRY(cudaFuncSetAttribute(write_rope_ring_kernel<D, FP8, Rows>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRopeRingBytes));
+                return PS_OK;
+            });
+            if (st != PS_OK) return st;
+            return launch_kernel(write_rope_ring_kernel<D, FP8, Rows>, tokens < kRopeRingCtas ? tokens : kRopeRingCtas, kRopeThreads + 32, kRopeStages * p.stage_bytes,
+                                 (cudaStream_t)stream, 1, true, p, rows);
+        };
+        if (pool.shape.dtype == 1) return launch(std::integral_constant<int, 128>{}, std::true_type{});
+        return d == 128 ? launch(std::integral_constant<int, 128>{}, std::false_type{}) : launch(std::integral_constant<int, 64>{}, std::false_type{});
     });
 }
 
