@@ -136,10 +136,14 @@ struct RopeLane {
         for (int i = 0; i < 4; ++i) unpack2(y[i], f[2 * i], f[2 * i + 1]);
         *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
     }
+    // the lane's part of a token in a bf16 page
+    __device__ __forceinline__ char* place(int g, int which, int64_t page, int slot) const {
+        return p.pool + (page * p.Hkv + g) * (int64_t)page_head_bytes(D) + which * block_bytes(D) + unit_offset(slot, e0);
+    }
     // The lane's part of a key (which = 0) or value (1) of kv head g to its page; by all lanes of a warp, some of which store nothing.
     __device__ __forceinline__ void store_kv(const uint64_t (&y)[4], int g, int which, int64_t page, int slot, bool yes) const {
         if (!FP8) {
-            if (yes) store16(p.pool + (page * p.Hkv + g) * (int64_t)page_head_bytes(D) + which * block_bytes(D) + unit_offset(slot, e0), y);
+            if (yes) store16(place(g, which, page, slot), y);
             return;
         }
         float f[8];
@@ -330,8 +334,12 @@ __global__ void __launch_bounds__(kRopeThreads + 32, 2) write_rope_ring_kernel(c
                 for (int g0 = first; g0 < p.Hkv; g0 += kStep) {
                     const int g = min(g0 + sub, p.Hkv - 1);
                     const uint4 x = *reinterpret_cast<const uint4*>(mine_at + q_bytes + kv_bytes + g * (2 * D));
-                    const uint64_t y[4] = {widened(x.x), widened(x.y), widened(x.z), widened(x.w)};
-                    mine.store_kv(y, g, 1, where.x, where.y, g == g0 + sub);
+                    if (FP8) {
+                        const uint64_t y[4] = {widened(x.x), widened(x.y), widened(x.z), widened(x.w)};
+                        mine.store_kv(y, g, 1, where.x, where.y, g == g0 + sub);
+                    } else if (g == g0 + sub) {
+                        *reinterpret_cast<uint4*>(mine.place(g, 1, where.x, where.y)) = x;
+                    }
                 }
             }
             __syncwarp();
