@@ -651,7 +651,7 @@ ps_status ps_kv_write_rope(ps_kv* kv, const ps_rope* a, const int32_t* block_tab
                 return PS_OK;
             });
             if (st != PS_OK) return st;
-            return launch_kernel(write_rope_ring_kernel<D, FP8, Rows>, tokens < kRopeRingCtas ? tokens : kRopeRingCtas, kRopeThreads + 32, kRopeStages * p.stage_bytes,
+            return launch_kernel(write_rope_ring_kernel<D, FP8, Rows>, kRopeRingCtas, kRopeThreads + 32, kRopeStages * p.stage_bytes,
                                  (cudaStream_t)stream, 1, true, p, rows);
         };
         if (pool.shape.dtype == 1) return launch(std::integral_constant<int, 128>{}, std::true_type{});

@@ -23,14 +23,15 @@
 //   warps 9, 10     MMA issue of streams 0 and 1: S = Q K^T (operands in shared memory) two steps ahead, into two buffers in turn,
 //                   O += P V (P as bf16 in the columns that S had), whichever's operands are there first
 //   warp 11         Q tiles; and V tiles that hold tree tokens or the sequence's end: rows behind the end become zero, and rows with
-//                   infinities or NaN too, because 0 * inf would reach nodes that do not see them; their weights are added by
+//                   infinities or NaN (FP8: or a scale over 255) too, because 0 * inf would reach nodes that do not see them; their weights are added by
 //                   the rows that do when the item ends.
 //
 // FP8 cache (E4M3 codes, a scale per token and kv head): half the bytes a key, so the conversion of the codes is what costs.  K's are
 // multiplied as they lie in the page: q 2^e (e of its row, the largest element in (224, 448]) is the sum of two E4M3 numbers, exactly
 // where an element has at least 2^-2 and within 2^-10 elsewhere, so S = Q1 K^T + Q2 K^T on the 8-bit tensor pipe, at the price
 // of one 16-bit product.  K's scales multiply the scores in fp32.  V becomes f16, code times half the scale (11 of at most 12 significant
-// bits; half, so that scales up to 255 stay in range), and the weights are rounded to f16.  Warp 11 converts Q, warps 12-15 V,
+// bits; half, so that scales up to 255 stay in range; as code / 256, exactly, times 128 scales, so that a scale's 8 bits lie in f16's normal range
+// down to 2^-21), and the weights are rounded to f16.  Warp 11 converts Q, warps 12-15 V,
 // in a ring of its own behind the copies'.
 //
 // Every wait is bounded; on expiry the CTA flags the pool and drains.
@@ -1059,14 +1060,14 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                     bool gone = false;
                     if (tree) {
                         auto nan = [](uint32_t c) { return (((c & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0; };
-                        const bool odd = key >= it.prior && key < it.kv_len && (nan(code.x) || nan(code.y) || nan(code.z) || nan(code.w) || !isfinite(vs));
+                        const bool odd = key >= it.prior && key < it.kv_len && (nan(code.x) || nan(code.y) || nan(code.z) || nan(code.w) || !(fabsf(vs) <= 255.f));
                         const uint32_t any = __ballot_sync(0xffffffffu, odd);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) flags |= (any >> (8 * k) & 0xffu ? 1u : 0u) << (4 * i + k);
                         gone = key >= it.kv_len || (any >> (lane & 24) & 0xffu);
                         if (gone) code = make_uint4(0, 0, 0, 0);
                     }
-                    const __half2 by = __float2half2_rn(gone ? 0.f : 0.5f * vs);
+                    const __half2 by = __float2half2_rn(gone ? 0.f : 128.f * vs), part = __float2half2_rn(1.f / 256.f);
                     const uint32_t c[4] = {code.x, code.y, code.z, code.w};
                     uint32_t y[8];
 #pragma unroll
@@ -1076,7 +1077,7 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                     }
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&y[k]), by);
+                        const __half2 v = __hmul2(__hmul2(*reinterpret_cast<const __half2*>(&y[k]), part), by);
                         y[k] = *reinterpret_cast<const uint32_t*>(&v);
                     }
                     // (the halves' lanes begin at different units: no bank conflicts)

@@ -167,3 +167,48 @@ def test_waits_that_run_out():
     again = c.pa.run_tree(q, c.table, mask, [700, 3000], [60, 33])
     c.pa.check_pool()
     assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+
+
+@pytest.mark.parametrize("power", [0, -6, -9, -12, -13])
+def test_small_values(power):
+    """V's scales down to the least that ps_shape names.
+
+    Beside the weights' rounding (2^-11 of each, and 2^-25 at the least of n weights of at most their sum), a value is code * scale / 2 in f16: the
+    scale's 8 bits are exact where scale * 2^7 is normal (else off by 2^-25 of at least 2^-15: 2^-10), the product is off by 2^-12 of itself
+    and 2^-25 at the least, 2^-24 of a value."""
+    prior, nodes = np.array([0, 0, 300, 40], dtype=np.int32), np.array([1, 2, 30, 64], dtype=np.int32)
+    c = Cache(8, 2, 128, prior + nodes, seed=34, fp8=True)
+    for r in range(4):
+        c.v[r] = (c.v[r].float() * 2.0 ** power).bfloat16()
+    c.fill()
+    mask, sees = tree_masks(nodes, 1, np.random.default_rng(2))
+    q = c.normal(int(nodes.sum()), 8, 128)
+    out, lse = c.pa.run_tree(q, c.table, mask, prior, nodes)
+    want, want_lse, bound, lse_bound = tree_reference(c, q, prior, sees)
+    largest = max(float(v.abs().max()) for v in c.v)
+    rest = bound - 2.0 ** -13 + (2.0 ** -12 + (2.0 ** -10 if power < -12 else 0) + int((prior + nodes).max()) * 2.0 ** -25) * largest + 2.0 ** -24
+    check_tree(out, lse, (want, want_lse, rest, lse_bound))
+
+
+def test_values_out_of_range_that_a_node_does_not_see():
+    """A drafted token's values beyond f16's range are finite, and have no part in the results of nodes that do not see it."""
+    import torch
+
+    prior, nodes = np.array([100], dtype=np.int32), np.array([20], dtype=np.int32)
+    c = Cache(8, 2, 128, prior + nodes, seed=35, fp8=True)
+    bad = [4, 11]
+    for i, v in zip(bad, (3e5, -2e38)):
+        c.v[0][100 + i, :, 5:7] = v
+    c.fill()
+    rng = np.random.default_rng(3)
+    mask, sees = tree_masks(nodes, 1, rng)
+    q = c.normal(20, 8, 128)
+    out, lse = c.pa.run_tree(q, c.table, mask, prior, nodes)
+    c.pa.check_pool()
+    touched = torch.from_numpy(sees[0][:, bad].any(1)).cuda()
+    assert bool(touched.any()) and not bool(touched.all())
+    assert bool(torch.isfinite(out[~touched]).all())
+    c.v[0][[104, 111]] = 0  # what is left is seen by the other rows
+    want, want_lse, bound, lse_bound = tree_reference(c, q, prior, sees)
+    rows = torch.nonzero(~touched).flatten()
+    check_tree(out[rows], lse[rows], (want[rows], want_lse[rows], bound[rows], lse_bound[rows]))
