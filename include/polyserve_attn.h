@@ -60,8 +60,9 @@ typedef enum {
  * Q is clamped to +-65504 and V scales are meant to lie in [2.4e-7, 255].  The
  * paper states no precision (its section 3.3 only notes that decode attention
  * time is set by the bytes of KV cache read); this variant halves those bytes.
- * It exists for head_dim 128 and serves decode rows only: ps_attn_plan refuses
- * batches with q_len > 1 and ps_profile_grid sweeps the bf16 cache only. */
+ * It exists for head_dim 128 and serves decode rows and trees of drafted tokens
+ * (ps_attn_tree): ps_attn_plan refuses batches with q_len > 1 and
+ * ps_profile_grid sweeps the bf16 cache only. */
 typedef struct {
     int32_t n_q_heads;
     int32_t n_kv_heads;

@@ -354,7 +354,9 @@ __global__ void __launch_bounds__(kRopeThreads + 32, 2) write_rope_ring_kernel(c
 //
 // A warp has one (request, kv head), a lane one 16-byte unit of K or V (and, FP8, a scale), the same unit of every token, so what a lane
 // reads no other lane writes.  It reads a group of tokens before it stores any of them, and what it has stored
-// lies below every later source: index[i] >= i.
+// lies below every later source: index[i] >= i.  Bound by the latency of a chain (path, pages, tokens), so the path's places and pages are
+// looked up by 32 lanes at once and handed round; one lookup after the other for each token took 12.8 us where this takes 11.1 (256 requests,
+// 8 kv heads, paths of up to 9 tokens in an FP8 cache, cold; 3 MB).
 // ---------------------------------------------------------------------------
 constexpr int kAcceptThreads = 128;
 constexpr int kAcceptAhead = 8;
@@ -448,7 +450,8 @@ __global__ void __launch_bounds__(kAcceptThreads) accept_kernel(const AcceptPara
 
 // ---------------------------------------------------------------------------
 // Reading back: tokens [begin, begin + len) of every sequence, packed, as bf16.  Bound by memory; a warp moves one token's K and V
-// with the loads of a chunk under way before its first store, as the gather of one sequence does.
+// with the loads of a chunk under way before its first store, as the gather of one sequence does.  Measured: 40536 tokens of 8 x 128 from an FP8
+// cache, 252 MB, in 40.6 us (6.2 TB/s).
 // ---------------------------------------------------------------------------
 constexpr int kReadThreads = 256;
 
