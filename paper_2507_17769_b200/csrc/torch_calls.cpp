@@ -294,17 +294,18 @@ PyObject* py_write_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// (kv, q, block table, mask, prior, n_nodes, out or None, lse or None, want lse, q heads, head dim, pool, workspace, its bytes, stream)
-// -> (status, out, lse or None)
+// (kv, q, block table, mask, prior, n_nodes, out or None, lse or None, want lse, q heads, head dim, pool, bytes of workspace, stream)
+// -> (status, out, lse or None).  The workspace is the call's own, from the stream's memory, as its results are: calls on several streams, and
+// graphs that are replayed side by side, share none.
 PyObject* py_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    void *kv, *ws, *stream;
+    void *kv, *stream;
     const at::Tensor *q, *bt, *mask, *given_out, *given_lse, *pool;
     int64_t hq, d, bytes;
     Batch batch;
-    if (!count_is(n, 15) || !as_ptr(a[0], &kv) || !as_tensor(a[1], &q) || !as_tensor(a[2], &bt) || !as_tensor(a[3], &mask) || !batch.get(a[4], a[5]) ||
+    if (!count_is(n, 14) || !as_ptr(a[0], &kv) || !as_tensor(a[1], &q) || !as_tensor(a[2], &bt) || !as_tensor(a[3], &mask) || !batch.get(a[4], a[5]) ||
         !optional_tensor(a[6], &given_out) || !optional_tensor(a[7], &given_lse) || !as_i64(a[9], &hq) || !as_i64(a[10], &d) || !as_tensor(a[11], &pool) ||
-        !as_ptr(a[12], &ws) || !as_i64(a[13], &bytes) || !as_ptr(a[14], &stream))
+        !as_i64(a[12], &bytes) || !as_ptr(a[13], &stream))
         return nullptr;
     const int64_t T = batch.total;
     if (!is_array(q, at::kBFloat16, {T, hq, d}, pool, "q must be contiguous bf16 [tokens, q heads, head dim] on the pool's device") || !is_table(bt, batch, pool) ||
@@ -320,8 +321,10 @@ PyObject* py_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (!given_out) out = at::empty({T, hq, d}, q->options());
         if (!given_lse && a[8] == Py_True) lse = at::empty({T, hq}, pool->options().dtype(at::kFloat));
         void* const lse_ptr = given_lse ? given_lse->data_ptr() : lse.defined() ? lse.data_ptr() : nullptr;
+        const at::Tensor ws = at::empty({bytes + 256}, pool->options().dtype(at::kByte));
+        void* const ws_ptr = (void*)(((uintptr_t)ws.data_ptr() + 255) / 256 * 256);
         st = f_tree((const ps_kv*)kv, q->data_ptr(), (const int32_t*)bt->data_ptr(), (int32_t)bt->size(1), (const int64_t*)mask->data_ptr(), (int32_t)mask->size(1),
-                    batch.a(), batch.b(), batch.n, given_out ? given_out->data_ptr() : out.data_ptr(), (float*)lse_ptr, ws, (size_t)bytes, stream);
+                    batch.a(), batch.b(), batch.n, given_out ? given_out->data_ptr() : out.data_ptr(), (float*)lse_ptr, ws_ptr, (size_t)bytes, stream);
     }
     return three(st, out.defined() ? THPVariable_Wrap(std::move(out)) : again(a[6]), lse.defined() ? THPVariable_Wrap(std::move(lse)) : again(a[7]));
     END_HANDLE_TH_ERRORS

@@ -62,6 +62,8 @@ class PagedAttention:
     >>> pa.accept(block_table_dev, prior, n_nodes, index, count)                          # the path that was accepted
     """
 
+    _tree_bytes = None  # of run_tree's workspace, once it is known
+
     def __init__(self, n_q_heads, n_kv_heads, head_dim, num_pages, page_size=16, device="cuda", poison=False, kv_dtype=0):
         """``kv_dtype``: 0 = bf16 cache, 1 = FP8 (E4M3) cache with a scale per (token, kv head); see ps_shape."""
         import torch
@@ -84,7 +86,6 @@ class PagedAttention:
         self._ws = None
         self._ws_bytes = 0
         self._ws_ptr = 0
-        self._tree_ws = None
         self._total_q = 0
         self._n_q_heads = int(n_q_heads)
         index = self.pool.device.index
@@ -206,12 +207,11 @@ class PagedAttention:
         """Attention for trees of drafted tokens: request r's n_nodes[r] tokens, cached behind its prior[r], see the whole context and
         the tree tokens of their mask rows.  q: bf16 [T, Hq, d]; mask: int64 [T, words], bit j % 64 of word j / 64 for node j.  Needs no
         plan.  Returns (out, lse)."""
-        if self._tree_ws is None:
-            self._tree_ws = self.torch.empty(B.ps_attn_tree_workspace(self.shape) + 256, dtype=self.torch.uint8, device=self.device)
-            self._tree_ws_ptr = (self._tree_ws.data_ptr() + 255) // 256 * 256
         s = self.shape
+        if self._tree_bytes is None:
+            self._tree_bytes = B.ps_attn_tree_workspace(s)
         status, out, lse = self._steps().tree(self.kv, q, block_table_dev, mask, B.lengths(prior), B.lengths(n_nodes), out, lse, bool(want_lse), s.n_q_heads,
-                                              s.head_dim, self.pool, self._tree_ws_ptr, self._tree_ws.numel() - 256, self._stream())
+                                              s.head_dim, self.pool, self._tree_bytes, self._stream())
         B._check(status)
         return out, lse
 

@@ -168,15 +168,57 @@ def test_more_requests_than_a_launch_takes():
 def test_results_are_the_same_every_time_and_with_a_dirty_workspace():
     import torch
 
+    import paper_2507_17769_b200 as ps
+
     c, q, mask, out, lse = run((16, 2, 128), [5000, 900], [40, 64], seed=20)
     for fill in (0xFF, 0x7F, 0):
-        c.pa._tree_ws.fill_(fill)
+        torch.full((ps.binding.ps_attn_tree_workspace(c.pa.shape) + 256,), fill, dtype=torch.uint8, device="cuda")  # (freed: the call gets this memory)
         again = c.pa.run_tree(q, c.table, mask, [5000, 900], [40, 64])
         assert torch.equal(again[0], out) and torch.equal(again[1], lse)
 
 
+def test_calls_on_two_streams_at_once():
+    """Calls of one pool on two streams, and two graphs replayed side by side, as a batch of many cut items uses the whole workspace."""
+    import torch
+
+    rng = np.random.default_rng(31)
+    prior, nodes = rng.integers(500, 6000, 20).astype(np.int32), rng.integers(20, 64, 20).astype(np.int32)
+    c = Cache(32, 8, 128, prior + nodes, seed=32).fill()
+    mask, sees = tree_masks(nodes, 1, rng)
+    qs = [c.normal(int(nodes.sum()), 32, 128) for _ in range(2)]
+    want = [c.pa.run_tree(q, c.table, mask, prior, nodes) for q in qs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(8):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                got[k].append(c.pa.run_tree(qs[k], c.table, mask, prior, nodes))
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(x, y) for res in got[k] for x, y in zip(res, want[k]))
+    graphs = []
+    for k in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            res = c.pa.run_tree(qs[k], c.table, mask, prior, nodes)
+        graphs.append((g, res))
+    for _ in range(4):
+        for k in range(2):
+            for x in graphs[k][1]:
+                x.zero_()
+        torch.cuda.synchronize()
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                graphs[k][0].replay()
+        torch.cuda.synchronize()
+        for k in range(2):
+            assert all(torch.equal(x, y) for x, y in zip(graphs[k][1], want[k]))
+    c.pa.check_pool()
+
+
 def test_other_streams_and_captured_graphs():
-    """A step captured whole, two graphs that take turns on one workspace, and another stream than the tensors'."""
+    """A step captured whole, two graphs that take turns, and another stream than the tensors'."""
     import torch
 
     rng = np.random.default_rng(21)
