@@ -8,6 +8,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 
 #include <cstdint>
 #include <cstring>
@@ -276,6 +277,7 @@ PyObject* py_write_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int st;
     {
         Unlocked u;
+        const c10::DeviceGuard there(pool->device());  // (a stream takes launches while its device is the current one)
         if (!given) out = at::empty({T, hq, d}, pool->options().dtype(at::kBFloat16));
         r.q_dev = q->data_ptr(), r.k_new_dev = k->data_ptr(), r.v_new_dev = v->data_ptr();
         r.q_out_dev = given ? given->data_ptr() : out.data_ptr();
@@ -318,6 +320,7 @@ PyObject* py_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int st;
     {
         Unlocked u;
+        const c10::DeviceGuard there(pool->device());  // (a stream takes launches while its device is the current one)
         if (!given_out) out = at::empty({T, hq, d}, q->options());
         if (!given_lse && a[8] == Py_True) lse = at::empty({T, hq}, pool->options().dtype(at::kFloat));
         void* const lse_ptr = given_lse ? given_lse->data_ptr() : lse.defined() ? lse.data_ptr() : nullptr;
@@ -345,6 +348,7 @@ PyObject* py_accept(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int st;
     {
         Unlocked u;
+        const c10::DeviceGuard there(pool->device());  // (a stream takes launches while its device is the current one)
         st = f_accept((ps_kv*)kv, (const int32_t*)bt->data_ptr(), (int32_t)bt->size(1), batch.a(), batch.b(), batch.n, (const int32_t*)index->data_ptr(),
                       (int32_t)index->size(1), (const int32_t*)count->data_ptr(), stream);
     }
@@ -367,6 +371,7 @@ PyObject* py_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int st;
     {
         Unlocked u;
+        const c10::DeviceGuard there(pool->device());  // (a stream takes launches while its device is the current one)
         const int64_t T = batch.total < 0 ? 0 : batch.total;
         const auto opts = pool->options().dtype(at::kBFloat16);
         k = at::empty({T, hkv, d}, opts), v = at::empty({T, hkv, d}, opts);
