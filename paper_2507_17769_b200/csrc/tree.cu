@@ -10,7 +10,7 @@
 //
 // Work: an item is one (request, kv head, group of up to 256 rows).  Its keys are tiles of 128, and all items' tiles, with
 // some more an item for its start and end, make one line that is cut into equal shares, a CTA each, wherever the cuts fall
-// (stream-K).  So one request on a long context, or a ragged batch, fills all SMs, and a CTA has at most two pieces of an item:
+// (stream-K); few and short items are a CTA each.  So one request on a long context, or a ragged batch, fills all SMs, and a CTA has at most two pieces of an item:
 // partial rows go to fixed places of the workspace and tree_merge_kernel joins them in the order of their keys.  The shares
 // follow from the batch's lengths, which travel as kernel parameters: there is no work list to upload and nothing to
 // initialise.
@@ -36,7 +36,7 @@
 //
 // Measured, with the merge kernel (32 q and 8 kv heads; floors at 6.56 TB/s): 32 trees of 11-32 nodes on 512-4096 tokens, 352 MB, 70 us (5.0 TB/s; floor 54);
 // FP8, 64 of 7-32, 352 MB, 151 us (floor 54); 8 heads of 64 without grouping, 24 of 20-61 on 300-5000, 128 MB, 43 us (floor 20); 64 of 48-64 on
-// 4096-12288, 610-670 us at the power cap (floor 378, of operations); one of 8 nodes on 700, 14 us.  Within an item bf16 of 128 dimensions runs at
+// 4096-12288, 610-670 us at the power cap (floor 378, of operations); one of 8 nodes on 700, 13 us.  Within an item bf16 of 128 dimensions runs at
 // HBM's rate.  The others are bound by the chain of a step: 1850 cycles (FP8 3200) for 64 keys of 128 rows, 1100 of them on exponentials, two
 // warps a scheduler, the rest tensor-memory loads and stores, fences and barriers.  An item's start and end cost some 8500 cycles
 // (64 dimensions 5400, FP8 15000), in which the loads get no further than the ring.
@@ -62,6 +62,12 @@ struct Cfg {
     // What an item's start and end cost, in key tiles.  Measured with 1 / 3 / 4 / 6 / 9: 32 trees of 11-32 nodes on 500-4000 tokens, 128 dimensions 76.0 /
     // 71.7 / 71.7 / 71.2 / 73.4 us; 24 of 20-61 on 300-5000, 64 dimensions 48.6 / 44.0 / 44.7 / 46.0 / 47.5; FP8, 64 of 7-32 on 500-4000 183 / 167 / 160 / 152 / 155.
     static constexpr int kItemUnits = FP8 ? 7 : D == 128 ? 5 : 3;
+    // Few and short items stay whole, a CTA each, where cutting would save fewer steps than joining the pieces costs; and a share has at least kLeastShare units.
+    // Measured, one tree of 8 nodes on 250 / 500 / 1000 / 1500 / 3000 tokens, whole and cut (32 q and 8 kv heads of 128): 7.7 / 9.8 / 13.6 / 17.4 /
+    // 29.4 and 11.4 / 12.6 / 13.9 / 14.3 / 17.4 us; FP8 17.6 / 20.2 / 26.1 / 32.3 / 50.9 and 18.4 / 23.0 / 24.0 / 24.8 / 27.9; 8 heads of 64 without grouping 6.6 /
+    // 8.5 / 12.1 / 15.7 / 26.9 and 11.2 / 13.5 / 14.3 / 15.5 / 19.3; of 64 nodes, two q tiles of 128, 13.8 / 17.9 / 25.4 / 32.8 / 54.7 and 18.1 / 19.9 / 21.2 / 21.9 / 26.2.
+    // (Shares of two units: 19.7 instead of 17.4 at 3000, 64 dimensions 25.8, of three 21.0, instead of 19.3.)
+    static constexpr int kMergeSteps = FP8 ? 3 : D == 128 ? 5 : 8, kLeastShare = D == 128 ? 3 : 4;
     static constexpr int kHalves = D / 64;
     static constexpr int kHalfBytes = kTileKeys * 128;
     static constexpr int kTileBytes = kHalves * kHalfBytes;  // a tile of Q, K or V in 16 bits
@@ -134,7 +140,9 @@ struct TreeParams {
     int* flag;
     int64_t num_pages;
     uint32_t wait_limit_ns;
-    int32_t max_pages, mask_words, n, Hq, Hkv, G, item_units, share, longer;  // a share's units; the first `longer` shares have one more
+    int32_t max_pages, mask_words, n, Hq, Hkv, G;
+    int32_t item_units;     // of an item beside its tiles; negative: -item_units in all, of every item, and a share is an item
+    int32_t share, longer;  // a share's units; the first `longer` shares have one more
 };
 
 // pieces of items in a CTA's share of the line
@@ -152,20 +160,23 @@ __device__ __forceinline__ int share_begin(const TreeParams& p, int c) { return 
 template <class Rows>
 struct PieceIter {
     const Rows& rows;
-    int G, Hkv, extra, left, r, head, group, w0;  // units of an item beside its tiles; units left of the share; where it goes on: request, kv head, group, units into the item
+    const TreeParams& p;
+    const int G, Hkv;  // (kept: read from the parameters at each use, FP8 takes 167 us instead of 151)
+    int left, r, head, group, w0;  // units left of the share; where it goes on: request, kv head, group, units into the item
     __device__ __forceinline__ int tiles() const { return (rows.prior[r] + rows.q_start[r + 1] - rows.q_start[r] + kTileKeys - 1) / kTileKeys; }
+    __device__ __forceinline__ int beside(int tiles) const { return p.item_units >= 0 ? p.item_units : -p.item_units - tiles; }
     __device__ __forceinline__ int groups(int nodes) const {
         const int shift = 31 - __clz(kGroupRows / G);  // (G is a power of two)
         return (nodes + (1 << shift) - 1) >> shift;
     }
-    __device__ __forceinline__ PieceIter(const Rows& rows_, int n, int G_, int Hkv_, int extra_, int u, int end) : rows(rows_), G(G_), Hkv(Hkv_), extra(extra_), left(end - u) {
-        int lo = 0, hi = n - 1;
+    __device__ __forceinline__ PieceIter(const Rows& rows_, const TreeParams& p_, int u, int end) : rows(rows_), p(p_), G(p_.G), Hkv(p_.Hkv), left(end - u) {
+        int lo = 0, hi = p.n - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (rows.unit_start[mid] <= u) lo = mid; else hi = mid - 1;
         }
         r = lo;
-        const int per = tiles() + extra, o = u - rows.unit_start[r], item = o / per, gr = groups(rows.q_start[r + 1] - rows.q_start[r]);
+        const int per = tiles() + beside(tiles()), o = u - rows.unit_start[r], item = o / per, gr = groups(rows.q_start[r + 1] - rows.q_start[r]);
         w0 = o - item * per;
         head = item / gr;
         group = item - head * gr;
@@ -179,6 +190,7 @@ struct PieceIter {
             x.kv_len = x.prior + x.nodes;
             x.tiles = tiles();
             x.head = head;
+            const int extra = beside(x.tiles);
             x.tile0 = max(0, w0 - extra);
             x.tile1 = max(0, min(x.tiles + extra, w0 + left) - extra);
             left -= x.tiles + extra - w0;
@@ -339,7 +351,7 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
     };
 
     constexpr uint32_t kColO = 256;
-    PieceIter<Rows> iter(rows, p.n, p.G, p.Hkv, C::kItemUnits, share_begin(p, blockIdx.x), share_begin(p, blockIdx.x + 1));
+    PieceIter<Rows> iter(rows, p, share_begin(p, blockIdx.x), share_begin(p, blockIdx.x + 1));
     Piece it;
     const int tile_tok = kRows / p.G, g_shift = 31 - __clz(p.G);
 
@@ -1234,21 +1246,28 @@ ps_status launch_rows(const TreeCall& a) {
     const int Hq = shape.n_q_heads, Hkv = shape.n_kv_heads, G = Hq / Hkv, group_tok = kGroupRows / G;
     using Rows = TreeRows<N>;
     Rows rows;  // (entries past n are not read)
-    int64_t units = 0;
-    int32_t tokens = 0;
-    bool wide = false;
+    auto tiles_of = [&](int r) { return ((int64_t)a.prior[r] + a.n_nodes[r] + kTileKeys - 1) / kTileKeys; };
+    auto items_of = [&](int r) { return Hkv * ((a.n_nodes[r] + group_tok - 1) / group_tok); };
+    int64_t units = 0, items = 0, longest = 0;
     for (int r = 0; r < a.n; ++r) {
-        rows.q_start[r] = tokens;
-        rows.unit_start[r] = (int32_t)units;
-        rows.prior[r] = a.prior[r];
-        tokens += a.n_nodes[r];
-        const int groups = (a.n_nodes[r] + group_tok - 1) / group_tok;
-        wide = wide || groups > 1;
-        units += (int64_t)Hkv * groups * (((int64_t)a.prior[r] + a.n_nodes[r] + kTileKeys - 1) / kTileKeys + Cfg<D, FP8>::kItemUnits);
+        items += items_of(r);
+        units += items_of(r) * (tiles_of(r) + Cfg<D, FP8>::kItemUnits);
+        longest = tiles_of(r) > longest ? tiles_of(r) : longest;
         if (units > 0x3fffffff) return fail(PS_ERR_INVALID, "too many keys in one batch");
     }
+    const int64_t fair = units / kSms > Cfg<D, FP8>::kLeastShare ? units / kSms : Cfg<D, FP8>::kLeastShare;
+    bool whole = items <= kSms;
+    for (int r = 0; whole && r < a.n; ++r) whole = (tiles_of(r) - fair) * (a.n_nodes[r] * G > kRows ? 2 : 1) <= Cfg<D, FP8>::kMergeSteps;
+    int32_t tokens = 0, begin = 0;
+    for (int r = 0; r < a.n; ++r) {
+        rows.q_start[r] = tokens;
+        rows.unit_start[r] = begin;
+        rows.prior[r] = a.prior[r];
+        tokens += a.n_nodes[r];
+        begin += (int32_t)(items_of(r) * (whole ? longest : tiles_of(r) + Cfg<D, FP8>::kItemUnits));
+    }
     rows.q_start[a.n] = tokens;
-    rows.unit_start[a.n] = (int32_t)units;
+    rows.unit_start[a.n] = begin;
 
     static PerDeviceOnce configured;
     const ps_status cfg = once_per_device(configured, []() -> ps_status {
@@ -1279,11 +1298,12 @@ ps_status launch_rows(const TreeCall& a) {
     p.flag = a.pool->flag_dev;
     p.num_pages = a.pool->num_pages;
     p.wait_limit_ns = (uint32_t)a.pool->wait_limit_ns;
-    p.max_pages = a.max_pages, p.mask_words = a.mask_words, p.n = a.n, p.Hq = Hq, p.Hkv = Hkv, p.G = G, p.item_units = Cfg<D, FP8>::kItemUnits;
-    const int grid = (int)(units / 2 < kSms ? units / 2 : kSms);
-    p.share = (int32_t)units / grid, p.longer = (int32_t)units % grid;
+    p.max_pages = a.max_pages, p.mask_words = a.mask_words, p.n = a.n, p.Hq = Hq, p.Hkv = Hkv, p.G = G, p.item_units = whole ? -(int32_t)longest : Cfg<D, FP8>::kItemUnits;
+    const int64_t cut = units / Cfg<D, FP8>::kLeastShare;
+    const int grid = (int)(whole ? items : cut < kSms ? cut : kSms);
+    p.share = begin / grid, p.longer = begin % grid;
     st = launch_kernel(tree_kernel<D, FP8, Rows>, grid, Cfg<D, FP8>::kThreads, Cfg<D, FP8>::kSmemBytes, a.stream, 1, true, p, q_map, pool_map, scale_map, rows);
-    if (st != PS_OK || grid == 1) return st;
+    if (st != PS_OK || whole) return st;
     return launch_kernel(tree_merge_kernel<D, Rows>, dim3(grid - 1, kGroupRows / (kMergeThreads / 32 * kMergeRows)), kMergeThreads, 0, a.stream, 1, true, p, rows);
 }
 

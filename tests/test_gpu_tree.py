@@ -305,3 +305,11 @@ def test_a_chain_is_a_chunk():
     ref, ref_lse = c.pa.run(q, c.table)
     c.pa.check()
     assert float((ref.float() - out.float()).abs().max()) <= 2e-2 and torch.allclose(lse, ref_lse, atol=2e-3)
+
+
+@pytest.mark.parametrize("heads,fp8", [((32, 8, 128), False), ((32, 8, 128), True), ((8, 8, 64), False), ((4, 2, 64), False)])
+@pytest.mark.parametrize("n,longest", [(1, 200), (3, 400), (9, 900), (18, 700), (18, 1500), (19, 700)])
+def test_few_items_whole_or_cut(heads, fp8, n, longest):
+    """Ragged batches on both sides of where items stay whole: by their count, and by their length."""
+    rng = np.random.default_rng(n + longest)
+    run(heads, rng.integers(0, longest, n), rng.integers(1, 65, n), seed=n, fp8=fp8)
