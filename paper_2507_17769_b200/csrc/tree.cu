@@ -679,8 +679,8 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
             const int32_t* bt = nullptr;
             it.tile1 = 0;
             bool have = true, ok = true;
-            // page of the next tile (lanes 0-7), requested a tile ahead of its use; -1: none, -2: the sequence has ended there
-            auto fetch = [&](int& page, int& kv_head, bool& tree) {
+            // pages of the next tile (lanes 0-7: as far as the sequence goes), requested a tile ahead of their use
+            auto fetch = [&](int& page, bool& inside, int& kv_head, bool& tree) {
                 if (j == it.tile1) {
                     have = iter.next(it);
                     if (!have) return;
@@ -689,14 +689,15 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                     bt = p.block_table + (int64_t)it.r * p.max_pages;
                 }
                 const int at = j * (kTileKeys / kPage) + lane;
-                page = lane < kTileKeys / kPage && at * kPage < it.kv_len ? __ldg(bt + at) : -2;
+                inside = lane < kTileKeys / kPage && at * kPage < it.kv_len;
+                page = inside ? __ldg(bt + at) : -1;
                 kv_head = head;
                 tree = j >= it.tree_tile();
                 ++j;
             };
-            auto pool_row = [&](int page, int kv_head) {
+            auto pool_row = [&](int page, bool inside, int kv_head) {
                 const bool good = (uint32_t)page < (uint64_t)p.num_pages;
-                if (!good && page != -2 && lane < kTileKeys / kPage) atomicOr(p.flag, kStatusBounds);
+                if (!good && inside) atomicOr(p.flag, kStatusBounds);
                 return good ? (page * p.Hkv + kv_head) * (FP8 ? 1 : 2 * C::kHalves) : -8;  // (rows outside the pool read as zero)
             };
             uint32_t n_raw = 0;
@@ -741,9 +742,9 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                 __syncwarp();
                 return true;
             };
-            int page = -2, kv_head = 0;
-            bool tree = false;
-            fetch(page, kv_head, tree);
+            int page = -1, kv_head = 0;
+            bool inside = false, tree = false;
+            fetch(page, inside, kv_head, tree);
             // K of tile n, then V of the one before
             int row_k = -8, row_v = -8;
             bool tree_v = false, more = have;
@@ -752,7 +753,7 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                     if (kv == 0) {
                         row_v = row_k;
                         if (!more) continue;
-                        row_k = pool_row(page, kv_head);
+                        row_k = pool_row(page, inside, kv_head);
                     } else if (n == 0) {
                         continue;
                     }
@@ -762,7 +763,7 @@ __global__ void __launch_bounds__(Cfg<D, FP8>::kThreads, 1) tree_kernel(const __
                 }
                 if (!more) break;
                 tree_v = tree;
-                fetch(page, kv_head, tree);
+                fetch(page, inside, kv_head, tree);
                 more = have;
             }
         } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
