@@ -215,7 +215,11 @@ __global__ void __launch_bounds__(kRopeThreads) write_rope_kernel(const RopePara
                 if (!is_v) mine.turn(y, xo, is_q ? mine.weighted(f, mine.wq, mine.wq_other) : mine.weighted(f, mine.wk, mine.wk_other), normed, rstd);
             }
             if (is_q) mine.store16(reinterpret_cast<char*>(p.q_out + ((int64_t)t * p.Hq + vec) * D + mine.e0), y);
-            if (!__all_sync(0xffffffffu, is_q)) mine.store_kv(y, vec - p.Hq - (is_v ? p.Hkv : 0), is_v, page, slot, !is_q && vec < n_vec);
+            if (!FP8 && is_v) {  // (as it came: through fp32 a NaN would lose its bits)
+                if (vec < n_vec) *reinterpret_cast<uint4*>(mine.place(vec - p.Hq - p.Hkv, 1, page, slot)) = x;
+            } else if (!FP8 || !__all_sync(0xffffffffu, is_q)) {
+                mine.store_kv(y, vec - p.Hq - (is_v ? p.Hkv : 0), is_v, page, slot, !is_q && vec < n_vec);
+            }
         }
     }
 }

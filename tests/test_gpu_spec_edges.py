@@ -5,6 +5,7 @@ import pytest
 import paper_2507_17769_b200 as ps
 from paper_2507_17769_b200 import binding as B
 from spec_util import Cache, tree_masks
+from test_gpu_spec_cache import angles
 
 pytestmark = pytest.mark.gpu
 
@@ -38,3 +39,26 @@ def test_every_page_outside_the_pool_is_reported(heads, fp8, entry):
     got = c.pa.run_tree(q, table, mask, prior, nodes)
     c.pa.check_pool()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("tokens", [1, 40, 296, 297, 900])
+@pytest.mark.parametrize("heads", [(8, 2, 128), (4, 2, 64)])
+def test_values_go_to_their_pages_bit_for_bit(tokens, heads):
+    """A NaN's sign and payload too, with few tokens as with many, and as write() stores them."""
+    import torch
+
+    hq, hkv, d = heads
+    c = Cache(hq, hkv, d, [tokens], seed=52)
+    x = c.normal(tokens, hq + 2 * hkv, d)
+    bits = x.view(torch.int16)
+    for i, b in enumerate((0x7FC1, -0x3D, 0x7F81, -0x7F, 0x7F80, -0x80, -0x8000, 1)):
+        bits[:, hq + hkv:, 3 + 7 * i] = b
+    w = torch.ones(d, device="cuda", dtype=torch.bfloat16)
+    v = x[:, hq + hkv:].contiguous()
+    for cos_sin, weight in ((None, None), (angles(tokens, d), w)):
+        c.pa.write_rope(x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:], c.table, [0], [tokens], cos_sin, q_weight=weight, k_weight=weight)
+        for got in (c.pa.gather(c.table[0], tokens)[1], c.pa.read(c.table, [0], [tokens])[1]):
+            assert torch.equal(got.view(torch.int16), v.view(torch.int16))
+        c.pa.pool.fill_(0xFF)
+    c.pa.write(x[:, hq:hq + hkv].contiguous(), v, c.table, [0], [tokens])
+    assert torch.equal(c.pa.gather(c.table[0], tokens)[1].view(torch.int16), v.view(torch.int16))
