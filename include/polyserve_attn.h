@@ -195,7 +195,8 @@ ps_status ps_kv_write_rope(ps_kv *kv, const ps_rope *args, const int32_t *block_
  * (mask_dev: [T, mask_words], mask_words in 1 .. 4; bits from n_nodes[r] on are
  * not looked at).  q, out and lse as for ps_attn_run, with T = sum n_nodes.  A
  * node that sees nothing gets zeros and lse = -inf.  What a node does not see
- * has no part in its result, whatever values it holds.
+ * has no part in its result, whatever values it holds.  out_dev, lse_out_dev and
+ * the workspace overlap neither each other nor an input (PS_ERR_INVALID).
  *
  * workspace_dev: 256-byte aligned device memory of
  * ps_attn_tree_workspace bytes, which depend on the shape alone; scratch, no

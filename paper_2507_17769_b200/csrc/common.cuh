@@ -122,6 +122,10 @@ struct KvPool {
 
 const KvPool& pool_of(const ps_kv* kv);
 
+inline bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {  // (nothing overlaps a range of no bytes)
+    return a_bytes > 0 && b_bytes > 0 && (uintptr_t)a < (uintptr_t)b + (uintptr_t)b_bytes && (uintptr_t)b < (uintptr_t)a + (uintptr_t)a_bytes;
+}
+
 // ---------------------------------------------------------------------------
 // device work list
 // ---------------------------------------------------------------------------

@@ -587,10 +587,6 @@ ps_status in_slices(const int32_t* prior, const int32_t* len, int32_t n, const F
     return PS_OK;
 }
 
-bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
-    return (uintptr_t)a < (uintptr_t)b + (uintptr_t)b_bytes && (uintptr_t)b < (uintptr_t)a + (uintptr_t)a_bytes;
-}
-
 }  // namespace
 
 }  // namespace ps

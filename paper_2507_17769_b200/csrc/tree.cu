@@ -1344,6 +1344,15 @@ ps_status ps_attn_tree(const ps_kv* kv, const void* q_dev, const int32_t* block_
         if (T > (1 << 24)) return fail(PS_ERR_INVALID, "more than 2^24 tokens in one batch");
     }
     const int64_t row = (int64_t)pool.shape.n_q_heads * pool.shape.head_dim;
+    // Results are stored while inputs are still read: queries and masks by other CTAs, and again by rows that see a V row taken out of the products.
+    const void* const read[3] = {q_dev, mask_dev, block_table_dev};
+    const void* const written[3] = {out_dev, lse_out_dev, workspace_dev};
+    const int64_t read_bytes[3] = {T * row * 2, T * mask_words * 8, (int64_t)n * max_pages * 4};
+    const int64_t written_bytes[3] = {T * row * 2, lse_out_dev ? T * pool.shape.n_q_heads * 4 : 0, (int64_t)workspace_bytes(pool.shape)};
+    for (int i = 0; i < 3; ++i)
+        for (int k = 0; k < 3; ++k)
+            if (overlap(written[i], written_bytes[i], read[k], read_bytes[k]) || (i < k && overlap(written[i], written_bytes[i], written[k], written_bytes[k])))
+                return fail(PS_ERR_INVALID, "out, lse and the workspace must not overlap each other or an input");
     int64_t t0 = 0;
     for (int32_t r0 = 0; r0 < n; r0 += kTreeRowsMax) {  // (a slice's kernel waits for the one before, whose workspace it uses)
         const int32_t m = n - r0 < kTreeRowsMax ? n - r0 : kTreeRowsMax;

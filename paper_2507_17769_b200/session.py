@@ -206,7 +206,7 @@ class PagedAttention:
     def run_tree(self, q, block_table_dev, mask, prior, n_nodes, out=None, lse=None, want_lse=True):
         """Attention for trees of drafted tokens: request r's n_nodes[r] tokens, cached behind its prior[r], see the whole context and
         the tree tokens of their mask rows.  q: bf16 [T, Hq, d]; mask: int64 [T, words], bit j % 64 of word j / 64 for node j.  Needs no
-        plan.  Returns (out, lse)."""
+        plan.  out, lse: default new tensors; they lie over no input.  Returns (out, lse)."""
         s = self.shape
         if self._tree_bytes is None:
             self._tree_bytes = B.ps_attn_tree_workspace(s)

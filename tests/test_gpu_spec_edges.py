@@ -62,3 +62,34 @@ def test_values_go_to_their_pages_bit_for_bit(tokens, heads):
         c.pa.pool.fill_(0xFF)
     c.pa.write(x[:, hq:hq + hkv].contiguous(), v, c.table, [0], [tokens])
     assert torch.equal(c.pa.gather(c.table[0], tokens)[1].view(torch.int16), v.view(torch.int16))
+
+
+def test_outputs_over_the_inputs_of_tree_attention_are_refused():
+    """Results are stored while inputs are still read."""
+    import torch
+
+    prior, nodes = np.array([40], dtype=np.int32), np.array([9], dtype=np.int32)
+    c = Cache(8, 2, 128, prior + nodes, seed=54).fill()
+    mask, _ = tree_masks(nodes, 1, np.random.default_rng(1))
+    room = c.normal(12, 8, 128)
+    q = room[:9]
+    want = c.pa.run_tree(q, c.table, mask, prior, nodes)
+    floats = room.view(-1).view(torch.float32)
+
+    def refused(**k):
+        assert status_of(lambda: c.pa.run_tree(q, c.table, mask, prior, nodes, **k)).status == B.PS_ERR_INVALID
+
+    before = room.clone()
+    refused(out=q)
+    refused(out=room[3:])
+    refused(lse=floats[:72].view(9, 8))
+    refused(lse=floats[9 * 512 - 8:9 * 512 + 64].view(9, 8))
+    both = torch.empty(9 * 8 * 128 + 144, dtype=torch.bfloat16, device="cuda")
+    refused(out=both[:9216].view(9, 8, 128), lse=both.view(torch.float32)[4600:4672].view(9, 8))
+    long = torch.zeros(9 * 1024 // 4, dtype=torch.int64, device="cuda")
+    long[2200:2209] = mask[:, 0]
+    assert status_of(lambda: c.pa.run_tree(q, c.table, long[2200:2209].view(9, 1), prior, nodes, out=long.view(torch.bfloat16).view(9, 8, 128))).status == B.PS_ERR_INVALID
+    assert torch.equal(room, before)
+    got = c.pa.run_tree(q, c.table, mask, prior, nodes, out=both[:9216].view(9, 8, 128), lse=both.view(torch.float32)[4608:4680].view(9, 8))  # side by side
+    c.pa.check_pool()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
