@@ -138,7 +138,8 @@ ps_status ps_kv_gather_fp8(const ps_kv *kv, const int32_t *block_table_row_dev, 
 
 /* Synchronises `stream`, then returns PS_OK, PS_ERR_BOUNDS or PS_ERR_TIMEOUT for
  * the kernels of the pool that have no plan (write, gather, the calls of a
- * speculative step) since the last call, and clears the flag. */
+ * speculative step) since the last call, and clears the flag.  Where several
+ * things went wrong it is PS_ERR_TIMEOUT, and ps_last_error names each. */
 ps_status ps_kv_status(ps_kv *kv, void *stream);
 
 /* ------------------------------------------------------------------------ */

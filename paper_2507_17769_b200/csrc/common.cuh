@@ -133,6 +133,7 @@ inline bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_byt
 constexpr int kPrefillRowsPerItem = 256;
 
 constexpr int kStatusOk = 0, kStatusBounds = 1, kStatusTimeout = 2;
+constexpr int kStatusAppendTimeout = 4;  // of a pool's flag only: a wait of an append ran out (a run's status has two bits, below its tag)
 
 // Device-side waits (on an mbarrier: a bulk copy landing, another warp's hand-over, an MMA group retiring) give up
 // after this long and flag the run instead of holding the GPU; ps_plan_set_wait_limit changes it per plan.

@@ -381,8 +381,13 @@ ps_status ps_kv_status(ps_kv* kv, void* stream) {
     PS_CUDA_TRY(cudaMemcpy(&flag, kv->p.flag_dev, sizeof flag, cudaMemcpyDeviceToHost));
     if (flag) {
         PS_CUDA_TRY(cudaMemset(kv->p.flag_dev, 0, sizeof flag));
-        if (flag & kStatusTimeout) return fail(PS_ERR_TIMEOUT, "a bounded wait inside the tree attention kernel expired; its output is invalid");
-        return fail(PS_ERR_BOUNDS, "a block-table entry pointed outside the pool, a position outside the table of angles, or an accepted path outside its tree; what it concerned was skipped");
+        const char* const outside = "a block-table entry pointed outside the pool, a position outside the table of angles, or an accepted path outside its tree; what it concerned was skipped";
+        const char* const append = "a bounded wait inside an append with norms and rotation expired; some of its tokens are missing from the cache and from q_out";
+        const char* const tree = "a bounded wait inside the tree attention kernel expired; its output is invalid";
+        const bool late = flag & (kStatusTimeout | kStatusAppendTimeout), both = (flag & kStatusTimeout) && (flag & kStatusAppendTimeout);
+        if (!late) return fail(PS_ERR_BOUNDS, "%s", outside);
+        return fail(PS_ERR_TIMEOUT, "%s%s%s%s%s", flag & kStatusAppendTimeout ? append : tree, both ? "; " : "", both ? tree : "", flag & kStatusBounds ? "; besides, " : "",
+                    flag & kStatusBounds ? outside : "");
     }
     return PS_OK;
 }

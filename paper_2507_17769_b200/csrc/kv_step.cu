@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(kRopeThreads + 32, 2) write_rope_ring_kernel(c
         __syncwarp();
         // what is under way lands before the block ends (as it does by itself where no wait ran out)
         for (int i = max(0, issued - kRopeStages); i < issued; ++i) mbar_wait(full + 8 * (i % kRopeStages), (i / kRopeStages) & 1, kDrainLimitNs);
-        if (!ok && lane == 0) atomicOr(p.flag, kStatusTimeout);
+        if (!ok && lane == 0) atomicOr(p.flag, kStatusAppendTimeout);
     } else {
         const RopeLane<D, FP8> mine(p);
         constexpr int kHeads = 32 / L;  // of a warp
@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(kRopeThreads + 32, 2) write_rope_ring_kernel(c
         uint32_t par = 0;
         for (int i = team; i < n; i += kRopeTeams) {
             if (!__all_sync(0xffffffffu, wait_or_abort(full + 8 * stage, par, s_abort))) {
-                if (lane == 0) atomicOr(p.flag, kStatusTimeout);
+                if (lane == 0) atomicOr(p.flag, kStatusAppendTimeout);
                 break;
             }
             const int2 where = s_where[stage];

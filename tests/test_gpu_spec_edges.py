@@ -5,7 +5,7 @@ import pytest
 import paper_2507_17769_b200 as ps
 from paper_2507_17769_b200 import binding as B
 from spec_util import Cache, tree_masks
-from test_gpu_spec_cache import angles
+from test_gpu_spec_cache import angles, append
 
 pytestmark = pytest.mark.gpu
 
@@ -93,3 +93,41 @@ def test_outputs_over_the_inputs_of_tree_attention_are_refused():
     got = c.pa.run_tree(q, c.table, mask, prior, nodes, out=both[:9216].view(9, 8, 128), lse=both.view(torch.float32)[4608:4680].view(9, 8))  # side by side
     c.pa.check_pool()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_what_went_wrong_is_named():
+    """A wait that ran out in the append is told apart from one in tree attention, and a bounds error beside one is told too."""
+    import torch
+
+    c, x, _ = append((8, 2, 128), [9], [700], 128, seed=53)
+    table = c.table.clone()
+    table[0, 1] = -1
+
+    def rope(bt=c.table):
+        c.pa.write_rope(x[:, :8], x[:, 8:10], x[:, 10:], bt, [9], [700], angles(709, 128))
+
+    def tree():
+        c.pa.run_tree(x[:5, :8].contiguous(), c.table, torch.ones((5, 1), dtype=torch.int64, device="cuda"), [100], [5])
+
+    def message(status):
+        e = status_of(c.pa.check_pool)
+        assert e.status == status
+        c.pa.check_pool()  # the report is given once
+        return str(e)
+
+    rope(table)
+    assert "outside the pool" in message(B.PS_ERR_BOUNDS)
+    for calls, words, others in (((rope,), ("append",), ("attention", "outside the pool")), ((tree,), ("tree attention",), ("append", "outside the pool")),
+                                 ((rope, tree), ("append", "tree attention"), ("outside the pool",))):
+        for with_bounds in (False, True):
+            if with_bounds:
+                rope(table)
+            ps.ps_kv_set_wait_limit(c.pa.kv, 0)
+            for f in calls:
+                f()
+            torch.cuda.synchronize()
+            ps.ps_kv_set_wait_limit(c.pa.kv, 2_000_000_000)
+            text = message(B.PS_ERR_TIMEOUT)
+            assert all(w in text for w in words), text
+            assert all(w not in text for w in others if not (with_bounds and w == "outside the pool")), text
+            assert ("outside the pool" in text) == with_bounds, text
