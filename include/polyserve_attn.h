@@ -170,7 +170,8 @@ typedef struct {
     const void *q_weight_dev;   /* bf16 [head_dim], or NULL: no norm */
     const void *k_weight_dev;
     const float *cos_sin_dev;   /* fp32 [n_positions, rot_dim] */
-    const int32_t *positions_dev; /* int32 [T], or NULL: position(t) is the token's position in its sequence */
+    /* int32 [T]: position(t), for a node of a drafted tree prior + its depth; NULL: the token's place in its sequence, prior + i */
+    const int32_t *positions_dev;
     int64_t n_positions;
     int32_t rot_dim;            /* a multiple of 16, at most head_dim; 0 = no rotation */
     int32_t interleaved;

@@ -57,7 +57,7 @@ class PagedAttention:
 
     A speculative step, whose new tokens are drafted trees:
 
-    >>> q = pa.write_rope(q, k, v, block_table_dev, prior, n_nodes, cos_sin, positions)   # norms, rotation, append
+    >>> q = pa.write_rope(q, k, v, block_table_dev, prior, n_nodes, cos_sin, positions)   # norms, rotation (a node's: prior + depth), append
     >>> out, lse = pa.run_tree(q, block_table_dev, mask, prior, n_nodes)                  # every node sees its ancestors
     >>> pa.accept(block_table_dev, prior, n_nodes, index, count)                          # the path that was accepted
     """
@@ -195,7 +195,8 @@ class PagedAttention:
 
         q [T, Hq, d], k_new and v_new [T, Hkv, d]: bf16, may be slices of one projection's output (heads packed, any token stride).
         cos_sin: float32 [positions, rot_dim], a row's cosines and then its sines, or None: no rotation; rot_dim is a multiple of 16.
-        positions: int32 [T], default the tokens' positions in their sequences.  q_weight, k_weight: bf16 [d], or None: no norm.
+        positions: int32 [T], the tokens' rows of cos_sin, default their places in the sequences, prior + i; a drafted tree's token
+        stands at its request's prior + its depth in the tree.  q_weight, k_weight: bf16 [d], or None: no norm.
         interleaved: pairs are neighbours instead of halves.  q_out: default a new tensor; q itself where it is packed."""
         s = self.shape
         status, q_out = self._steps().write_rope(self.kv, q, k_new, v_new, block_table_dev, B.lengths(prior), B.lengths(q_len), cos_sin, positions, q_weight,

@@ -1,13 +1,18 @@
 """Calls of a speculative step at the edges of what their documentation allows."""
+import glob
+import os
+
 import numpy as np
 import pytest
 
 import paper_2507_17769_b200 as ps
 from paper_2507_17769_b200 import binding as B
 from spec_util import Cache, tree_masks
-from test_gpu_spec_cache import angles, append
+from test_gpu_spec_cache import angles, append, check_rounded, turned
 
 pytestmark = pytest.mark.gpu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 def status_of(f):
@@ -131,3 +136,29 @@ def test_what_went_wrong_is_named():
             assert all(w in text for w in words), text
             assert all(w not in text for w in others if not (with_bounds and w == "outside the pool")), text
             assert ("outside the pool" in text) == with_bounds, text
+
+
+def test_the_documented_step():
+    """The example of a speculative step in the documentation, as it stands there: drafted tokens are rotated by their positions in their sequences."""
+    import torch
+
+    (path,) = glob.glob(os.path.join(ROOT, "READ*"))
+    blocks = open(path).read().split("```python\n")[1:]
+    code = [b.split("```")[0] for b in blocks if "write_rope(" in b]
+    assert len(code) == 1
+    prior, n_nodes = np.array([50, 0, 7], dtype=np.int32), np.array([9, 1, 20], dtype=np.int32)
+    pa_cache = Cache(8, 2, 128, prior + n_nodes, seed=55).fill()
+    mask, sees = tree_masks(n_nodes, 1, np.random.default_rng(2))
+    depth = np.concatenate([s.sum(1) - 1 for s in sees]).astype(np.int32)
+    x = pa_cache.normal(30, 12, 128)
+    qw, kw = ((1 + 0.3 * torch.randn(128, generator=pa_cache.gen, device="cuda")).bfloat16() for _ in range(2))
+    table = angles(64, 128)
+    names = dict(pa=pa_cache.pa, q=x[:, :8], k_new=x[:, 8:10], v_new=x[:, 10:], block_table=pa_cache.table, prior=prior, n_nodes=n_nodes, cos_sin=table,
+                 depth=torch.from_numpy(depth).cuda(), qw=qw, kw=kw, mask=mask, index=torch.zeros((3, 1), dtype=torch.int32, device="cuda"),
+                 count=torch.ones(3, dtype=torch.int32, device="cuda"), begin=prior, length=n_nodes, np=np, torch=torch)
+    exec(compile(code[0], "example", "exec"), names)
+    pa_cache.pa.check_pool()
+    pos = torch.from_numpy(np.repeat(prior, n_nodes) + depth).cuda().long()
+    check_rounded(names["q"], *turned(x[:, :8], qw, 1e-6, table, pos, False))
+    check_rounded(names["k"], *turned(x[:, 8:10], kw, 1e-6, table, pos, False))
+    assert torch.equal(names["v"], x[:, 10:])
