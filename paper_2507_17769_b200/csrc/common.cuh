@@ -122,6 +122,9 @@ struct KvPool {
 
 const KvPool& pool_of(const ps_kv* kv);
 
+// Tokens of a sequence, at the most: kernels hold positions, and keys rounded up to tiles, in 32 bits.
+constexpr int64_t kMaxTokens = 0x7fffffff - 255;
+
 inline bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {  // (nothing overlaps a range of no bytes)
     return a_bytes > 0 && b_bytes > 0 && (uintptr_t)a < (uintptr_t)b + (uintptr_t)b_bytes && (uintptr_t)b < (uintptr_t)a + (uintptr_t)a_bytes;
 }

@@ -330,6 +330,7 @@ ps_status ps_kv_write(ps_kv* kv, const void* k_new_dev, const void* v_new_dev, c
             return fail(PS_ERR_INVALID, "request %d: q_len=%d prior=%d", r, q_len_host[r], prior_host[r]);
         if ((int64_t)prior_host[r] + q_len_host[r] > (int64_t)max_pages * kPage)
             return fail(PS_ERR_INVALID, "request %d: kv_len exceeds max_pages * page_size", r);
+        if ((int64_t)prior_host[r] + q_len_host[r] > kMaxTokens) return fail(PS_ERR_INVALID, "request %d: more than %lld tokens", r, (long long)kMaxTokens);
         T += q_len_host[r];
         if (T > 0x7fffffffLL / 64) return fail(PS_ERR_INVALID, "too many new tokens");
     }

@@ -549,6 +549,7 @@ ps_status check_lengths(int32_t max_pages, const int32_t* prior, const int32_t* 
     for (int r = 0; r < n; ++r) {
         if (len[r] < least || prior[r] < 0) return fail(PS_ERR_INVALID, "request %d: %d tokens behind %d", r, len[r], prior[r]);
         if ((int64_t)prior[r] + len[r] > (int64_t)max_pages * kPage) return fail(PS_ERR_INVALID, "request %d: its tokens exceed max_pages * page_size", r);
+        if ((int64_t)prior[r] + len[r] > kMaxTokens) return fail(PS_ERR_INVALID, "request %d: more than %lld tokens", r, (long long)kMaxTokens);
         T += len[r];
         if (T > 0x7fffffffLL / 64) return fail(PS_ERR_INVALID, "too many tokens");
     }

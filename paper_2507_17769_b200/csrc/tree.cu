@@ -1340,6 +1340,7 @@ ps_status ps_attn_tree(const ps_kv* kv, const void* q_dev, const int32_t* block_
         if (prior_host[r] < 0 || n_nodes_host[r] < 1) return fail(PS_ERR_INVALID, "request %d: %d nodes behind %d tokens", r, n_nodes_host[r], prior_host[r]);
         if (n_nodes_host[r] > 64 * mask_words) return fail(PS_ERR_INVALID, "request %d: %d nodes in a mask of %d bits", r, n_nodes_host[r], 64 * mask_words);
         if ((int64_t)prior_host[r] + n_nodes_host[r] > (int64_t)max_pages * kPage) return fail(PS_ERR_INVALID, "request %d: its tokens exceed max_pages * page_size", r);
+        if ((int64_t)prior_host[r] + n_nodes_host[r] > kMaxTokens) return fail(PS_ERR_INVALID, "request %d: more than %lld tokens", r, (long long)kMaxTokens);
         T += n_nodes_host[r];
         if (T > (1 << 24)) return fail(PS_ERR_INVALID, "more than 2^24 tokens in one batch");
     }

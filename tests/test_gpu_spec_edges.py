@@ -162,3 +162,27 @@ def test_the_documented_step():
     check_rounded(names["q"], *turned(x[:, :8], qw, 1e-6, table, pos, False))
     check_rounded(names["k"], *turned(x[:, 8:10], kw, 1e-6, table, pos, False))
     assert torch.equal(names["v"], x[:, 10:])
+
+
+def test_positions_beyond_32_bits_are_refused():
+    """... by every call, however wide the block table: kernels count them in 32 bits."""
+    import torch
+
+    pa = ps.PagedAttention(8, 2, 128, 8)
+    x = torch.zeros((512, 12, 128), dtype=torch.bfloat16, device="cuda")
+    some = torch.zeros(1 << 16, dtype=torch.int32, device="cuda")
+    ws = torch.empty(B.ps_attn_tree_workspace(pa.shape) + 256, dtype=torch.uint8, device="cuda")
+    at = (ws.data_ptr() + 255) // 256 * 256
+    q, out = (torch.zeros((256, 8, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    k = torch.zeros((256, 2, 128), dtype=torch.bfloat16, device="cuda")
+    rope = B.ps_rope(q_dev=x.data_ptr(), k_new_dev=x.data_ptr() + 2048, v_new_dev=x.data_ptr() + 2560, q_out_dev=out.data_ptr(), q_stride=1536, k_stride=1536, v_stride=1536)
+    pages = 2 ** 27 + 32  # 2^31 + 512 tokens
+    calls = {"write": lambda a, b: B.ps_kv_write(pa.kv, k, k, some, pages, a, b), "write_rope": lambda a, b: B.ps_kv_write_rope(pa.kv, rope, some, pages, a, b),
+             "run_tree": lambda a, b: B.ps_attn_tree(pa.kv, q, some, pages, some, 4, a, b, out, None, at, ws.numel() - 256),
+             "accept": lambda a, b: B.ps_kv_accept(pa.kv, some, pages, a, b, some, 4, some), "read": lambda a, b: B.ps_kv_read(pa.kv, some, pages, a, b, k, k),
+             "plan": lambda a, b: B.ps_attn_plan(pa.shape, a, b, pages)}
+    for name, call in calls.items():
+        for prior, length in ((2 ** 31 - 8, 16), (2 ** 31 - 1, 1), (2 ** 31 - 200, 200), (2 ** 31 - 256, 1)):
+            e = status_of(lambda: call([prior], [length]))
+            assert e.status == B.PS_ERR_INVALID and "more than" in str(e), (name, prior, length, str(e))
+    pa.check_pool()
