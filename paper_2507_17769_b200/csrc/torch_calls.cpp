@@ -372,11 +372,17 @@ PyObject* py_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     {
         Unlocked u;
         const c10::DeviceGuard there(pool->device());  // (a stream takes launches while its device is the current one)
-        const int64_t T = batch.total < 0 ? 0 : batch.total;
-        const auto opts = pool->options().dtype(at::kBFloat16);
-        k = at::empty({T, hkv, d}, opts), v = at::empty({T, hkv, d}, opts);
-        st = f_read((const ps_kv*)kv, (const int32_t*)bt->data_ptr(), (int32_t)bt->size(1), batch.a(), batch.b(), batch.n, k.data_ptr(), v.data_ptr(), stream);
+        const auto read = [&](void* k_out, void* v_out) {
+            return f_read((const ps_kv*)kv, (const int32_t*)bt->data_ptr(), (int32_t)bt->size(1), batch.a(), batch.b(), batch.n, k_out, v_out, stream);
+        };
+        st = read(nullptr, nullptr);  // (the library's checks: lengths that it refuses may ask for any amount of memory)
+        if (st == PS_OK) {
+            const auto opts = pool->options().dtype(at::kBFloat16);
+            k = at::empty({batch.total, hkv, d}, opts), v = at::empty({batch.total, hkv, d}, opts);
+            st = read(k.data_ptr(), v.data_ptr());
+        }
     }
+    if (!k.defined()) return three(st, again(Py_None), again(Py_None));
     return three(st, THPVariable_Wrap(std::move(k)), THPVariable_Wrap(std::move(v)));
     END_HANDLE_TH_ERRORS
 }

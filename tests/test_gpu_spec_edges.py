@@ -186,3 +186,13 @@ def test_positions_beyond_32_bits_are_refused():
             e = status_of(lambda: call([prior], [length]))
             assert e.status == B.PS_ERR_INVALID and "more than" in str(e), (name, prior, length, str(e))
     pa.check_pool()
+
+
+def test_lengths_are_refused_before_results_are_allocated():
+    """2^31 - 1 tokens a request would be half a terabyte of K."""
+    import torch
+
+    pa = ps.PagedAttention(8, 2, 128, 4)
+    table = torch.zeros((2, 4), dtype=torch.int32, device="cuda")
+    for length in ([2 ** 31 - 1, 1], [2 ** 31 - 1, 2 ** 31 - 1], [65, 0], [2 ** 31 - 1, -1]):
+        assert status_of(lambda: pa.read(table, [0, 0], length)).status == B.PS_ERR_INVALID
