@@ -27,6 +27,8 @@ constexpr int kRopeAhead = 3;     // few tokens: heads of a lane whose loads are
 // Many tokens: four stages a CTA and two CTAs an SM.  (32 + 8 + 8 heads, bf16: 3000 tokens take 18.8 us with four stages and two teams of
 // four warps, 17.8 with eight stages and four teams of two, but 6722 tokens 36 us against 39; one team of eight warps 23.1, a warp a token 28.)
 constexpr int kRopeStages = 4, kRopeTeams = 2, kRopeTeamWarps = kRopeThreads / 32 / kRopeTeams;
+// (Tokens of which four do not fit, from some 100 heads of 128 in all, take a CTA each at any count, at a price: 6000 tokens of 80 + 10 + 10 heads in stretches 60 us,
+// 5.2 TB/s; of 96 + 12 + 12 a CTA each 133 us, 2.8 TB/s.)
 constexpr int kRopeRingBytes = 108 * 1024, kRopeRingCtas = 2 * 148;
 // Up to here a CTA a token is faster: all of them run at once and none waits for a stage.  (The same heads, a CTA a token and in
 // stretches: 64 tokens 3.4 and 5.9 us, 256 4.1 and 6.6, 400 7.3 and 6.0, 900 12.5 and 8.8; FP8 256 4.7 and 8.1, 400 8.3 and 7.0.)

@@ -34,12 +34,14 @@
 // down to 2^-21), and the weights are rounded to f16.  Warp 11 converts Q, warps 12-15 V,
 // in a ring of its own behind the copies'.
 //
-// Measured, with the merge kernel (32 q and 8 kv heads; floors at 6.56 TB/s): 32 trees of 11-32 nodes on 512-4096 tokens, 352 MB, 70 us (5.0 TB/s; floor 54);
-// FP8, 64 of 7-32, 352 MB, 151 us (floor 54); 8 heads of 64 without grouping, 24 of 20-61 on 300-5000, 128 MB, 43 us (floor 20); 64 of 48-64 on
-// 4096-12288, 610-670 us at the power cap (floor 378, of operations); one of 8 nodes on 700, 13 us.  Within an item bf16 of 128 dimensions runs at
-// HBM's rate.  The others are bound by the chain of a step: 1850 cycles (FP8 3200) for 64 keys of 128 rows, 1100 of them on exponentials, two
-// warps a scheduler, the rest tensor-memory loads and stores, fences and barriers.  An item's start and end cost some 8500 cycles
-// (64 dimensions 5400, FP8 15000), in which the loads get no further than the ring.
+// Measured, with the merge kernel (32 q and 8 kv heads; floors, all of bytes, at 6.56 TB/s), in calls one after the other for 15 ms / for more than a second, when
+// 128 dimensions run at the power cap: 32 trees of 11-32 nodes on 512-4096 tokens, 352 MB, 70 / 79 us (5.0 / 4.5 TB/s; floor 54; 1.96 / 1.55 GHz); FP8, 64 of 7-32,
+// 352 MB, 152 / 161 us (floor 54); 8 heads of 64 without grouping, 24 of 20-61 on 300-5000, 128 MB, 43 us (floor 20); 64 of 48-64 on 4096-12288, 2.48 GB,
+// 640 / 746 us (floor 378; operations 327; 1.45 GHz); one of 8 nodes on 700, 13 us.  Within an item bf16 of 128 dimensions runs at HBM's rate.  The others are
+// bound by the chain of a step: 1850 cycles (FP8 3200) for 64 keys of 128 rows, 1100 of them on exponentials, two warps a scheduler, the rest tensor-memory loads
+// and stores, fences and barriers.  (With at most 64 rows both streams' rows lie in the same 64 lanes, so two of the four schedulers have all of them; and the FP8
+// form's 16 warps have 128 registers each, of which the softmax spills 29 words.)  An item's start and end cost some 8500 cycles (64 dimensions 5400, FP8 15000),
+// in which the loads get no further than the ring.
 //
 // Every wait is bounded; on expiry the CTA flags the pool and drains.
 #include <cuda_fp16.h>
