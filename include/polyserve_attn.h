@@ -163,7 +163,7 @@ typedef struct {
     const void *q_dev;          /* bf16, token t at q_dev + t * q_stride: [n_q_heads, head_dim] */
     const void *k_new_dev;      /* bf16 [n_kv_heads, head_dim] a token */
     const void *v_new_dev;      /* bf16 [n_kv_heads, head_dim] a token */
-    void *q_out_dev;            /* bf16 [T, n_q_heads, head_dim]; may be q_dev itself where that is packed */
+    void *q_out_dev;            /* bf16 [T, n_q_heads, head_dim]; may be q_dev itself where that is packed, else over no input */
     int64_t q_stride;           /* elements from one token to the next, a multiple of 8; 0 = packed */
     int64_t k_stride;
     int64_t v_stride;
@@ -230,7 +230,8 @@ ps_status ps_kv_accept(ps_kv *kv, const int32_t *block_table_dev, int32_t max_pa
 
 /*
  * Read tokens begin[r] .. begin[r] + len[r] (len >= 0) of n sequences back, packed as
- * bf16 [sum len, n_kv_heads, head_dim] (either output may be NULL): a bf16 pool's
+ * bf16 [sum len, n_kv_heads, head_dim] (either output may be NULL; they overlap
+ * neither each other nor the block table): a bf16 pool's
  * bit for bit, an FP8 pool's as code * scale rounded to bf16.  Tokens whose page
  * lies outside the pool are left unwritten and reported by ps_kv_status.
  */

@@ -624,6 +624,11 @@ ps_status ps_kv_write_rope(ps_kv* kv, const ps_rope* a, const int32_t* block_tab
         if (!in_place && overlap(a->q_out_dev, T * widths[0] * 2, in[i], ((T - 1) * strides[i] + widths[i]) * 2))
             return fail(PS_ERR_INVALID, "q_out overlaps an input (it may be q itself where q is packed)");
     }
+    // (what other tokens read while a token's queries are stored)
+    const void* const shared[5] = {a->q_weight_dev, a->k_weight_dev, a->rot_dim > 0 ? a->cos_sin_dev : nullptr, a->positions_dev, block_table_dev};
+    const int64_t bytes[5] = {d * 2, d * 2, a->n_positions * a->rot_dim * 4, T * 4, (int64_t)n * max_pages * 4};
+    for (int i = 0; i < 5; ++i)
+        if (shared[i] && overlap(a->q_out_dev, T * widths[0] * 2, shared[i], bytes[i])) return fail(PS_ERR_INVALID, "q_out overlaps an input (it may be q itself where q is packed)");
     return in_slices(prior_host, q_len_host, n, [&](const auto& rows, int32_t r0, int64_t t0, int32_t m, int32_t tokens) {
         using Rows = std::decay_t<decltype(rows)>;
         RopeParams p;
@@ -699,6 +704,10 @@ ps_status ps_kv_read(const ps_kv* kv, const int32_t* block_table_dev, int32_t ma
     if (!k_out_dev && !v_out_dev) return PS_OK;
     const KvPool& pool = pool_of(kv);
     const int Hkv = pool.shape.n_kv_heads, d = pool.shape.head_dim;
+    const int64_t out_bytes = T * Hkv * d * 2, table_bytes = (int64_t)n * max_pages * 4;
+    if ((k_out_dev && v_out_dev && overlap(k_out_dev, out_bytes, v_out_dev, out_bytes)) || (k_out_dev && overlap(k_out_dev, out_bytes, block_table_dev, table_bytes)) ||
+        (v_out_dev && overlap(v_out_dev, out_bytes, block_table_dev, table_bytes)))
+        return fail(PS_ERR_INVALID, "the outputs overlap each other or the block table");
     const bool aligned = (((uintptr_t)k_out_dev | (uintptr_t)v_out_dev) & 31) == 0;
     return in_slices(begin_host, len_host, n, [&](const auto& rows, int32_t r0, int64_t t0, int32_t m, int32_t tokens) {
         using Rows = std::decay_t<decltype(rows)>;

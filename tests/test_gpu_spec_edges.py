@@ -196,3 +196,64 @@ def test_lengths_are_refused_before_results_are_allocated():
     table = torch.zeros((2, 4), dtype=torch.int32, device="cuda")
     for length in ([2 ** 31 - 1, 1], [2 ** 31 - 1, 2 ** 31 - 1], [65, 0], [2 ** 31 - 1, -1]):
         assert status_of(lambda: pa.read(table, [0, 0], length)).status == B.PS_ERR_INVALID
+
+
+def test_outputs_over_the_inputs_of_the_cache_calls_are_refused():
+    """What a call reads for other tokens must not change while one token's results are stored."""
+    import torch
+
+    c = Cache(2, 1, 64, [32], seed=56).fill()
+    x = c.normal(32, 4, 64)
+    room = torch.zeros(3 * 32 * 128, dtype=torch.bfloat16, device="cuda")
+    out = room[4096:8192].view(32, 2, 64)
+    w, cs, pos = torch.ones(64, dtype=torch.bfloat16, device="cuda"), angles(32, 64), torch.arange(32, dtype=torch.int32, device="cuda")
+    good = dict(cos_sin=cs, positions=pos, q_weight=w, k_weight=w, block_table_dev=c.table)
+    inside = {"cos_sin": room[1024:5120].view(torch.float32).view(32, 64), "positions": room[8000:8064].view(torch.int32), "q_weight": room[8176:8240], "k_weight": room[4040:4104],
+              "block_table_dev": room[4092:4092 + 2 * c.table.numel()].view(torch.int32).view(c.table.shape)}
+
+    def call(**k):
+        k = {**good, **k}
+        return c.pa.write_rope(x[:, :2], x[:, 2:3], x[:, 3:], k.pop("block_table_dev"), [0], [32], q_out=out, **k)
+
+    for name, t in inside.items():
+        t.copy_(good[name])
+        assert status_of(lambda: call(**{name: t})).status == B.PS_ERR_INVALID, name
+    beside = {"cos_sin": room[:4096].view(torch.float32).view(32, 64), "positions": room[8192:8256].view(torch.int32), "q_weight": room[8256:8320], "k_weight": room[8320:8384],
+              "block_table_dev": room[8384:8384 + 2 * c.table.numel()].view(torch.int32).view(c.table.shape)}
+    want = c.pa.write_rope(x[:, :2], x[:, 2:3], x[:, 3:], c.table, [0], [32], cs, positions=pos, q_weight=w, k_weight=w)
+    for name, t in beside.items():
+        t.copy_(good[name])
+    assert torch.equal(call(**beside), want)
+    k, v = (torch.empty(32, 1, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table = beside["block_table_dev"]
+    over = room[8320:8320 + 2048]
+    for a, b, bt in ((k, k, c.table), (over, v, table), (k, over, table), (None, over, table), (room[:2048], room[2040:4088], c.table)):
+        assert status_of(lambda: B.ps_kv_read(c.pa.kv, bt, bt.size(1), [0], [32], a, b)).status == B.PS_ERR_INVALID
+    B.ps_kv_read(c.pa.kv, table, table.size(1), [0], [32], room[:2048], room[2048:4096])
+    c.pa.check_pool()
+    assert torch.equal(room[:2048].view(32, 1, 64), c.pa.read(c.table, [0], [32])[0]) and torch.equal(room[2048:4096].view(32, 1, 64), x[:, 3:])
+
+
+@pytest.mark.parametrize("heads,fp8", [((2, 1, 64), False), ((2, 2, 128), True)])
+def test_paths_and_stretches_of_more_requests_than_a_launch_takes(heads, fp8):
+    import torch
+
+    n = 8100
+    rng = np.random.default_rng(57)
+    prior, nodes = rng.integers(0, 20, n).astype(np.int32), rng.integers(1, 6, n).astype(np.int32)
+    c = Cache(*heads, prior + nodes, seed=58, fp8=fp8).fill()
+    index = np.full((n, 3), -7, dtype=np.int32)
+    count = np.minimum(rng.integers(0, 4, n), nodes).astype(np.int32)
+    for r in range(n):
+        index[r, :count[r]] = np.sort(rng.choice(nodes[r], count[r], replace=False))
+    start = np.cumsum(prior + nodes) - prior - nodes
+    source = np.arange(int((prior + nodes).sum()))
+    for r in range(n):
+        at = start[r] + prior[r]
+        source[at:at + count[r]] = at + index[r, :count[r]]
+    before = c.pa.read(c.table, np.zeros(n, dtype=np.int32), prior + nodes)
+    c.pa.accept(c.table, prior, nodes, torch.from_numpy(index).cuda(), torch.from_numpy(count).cuda())
+    after = c.pa.read(c.table, np.zeros(n, dtype=np.int32), prior + nodes)
+    c.pa.check_pool()
+    assert torch.equal(before[0], torch.cat(c.k).bfloat16()) and torch.equal(before[1], torch.cat(c.v).bfloat16())
+    assert all(torch.equal(b, a[torch.from_numpy(source).cuda()]) for a, b in zip(before, after))
