@@ -8,7 +8,7 @@ import pytest
 import paper_2507_17769_b200 as ps
 from paper_2507_17769_b200 import binding as B
 from spec_util import Cache, tree_masks
-from test_gpu_spec_cache import angles, append, check_rounded, turned
+from test_gpu_spec_cache import angles, append, check_fp8, check_rounded, turned
 
 pytestmark = pytest.mark.gpu
 
@@ -257,3 +257,27 @@ def test_paths_and_stretches_of_more_requests_than_a_launch_takes(heads, fp8):
     c.pa.check_pool()
     assert torch.equal(before[0], torch.cat(c.k).bfloat16()) and torch.equal(before[1], torch.cat(c.v).bfloat16())
     assert all(torch.equal(b, a[torch.from_numpy(source).cuda()]) for a, b in zip(before, after))
+
+
+@pytest.mark.parametrize("tokens", [40, 700])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("which", ["q", "k"])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_a_norm_of_queries_or_of_keys_alone(tokens, interleaved, which, fp8):
+    import torch
+
+    c = Cache(8, 2, 128, [tokens], seed=59, fp8=fp8)
+    x = c.normal(tokens, 12, 128, scale=3.0)
+    w = (1 + 0.3 * torch.randn(128, generator=c.gen, device="cuda")).bfloat16()
+    weight = {"q": None, "k": None, which: w}
+    table = angles(tokens, 96)
+    q = c.pa.write_rope(x[:, :8], x[:, 8:10], x[:, 10:], c.table, [0], [tokens], table, q_weight=weight["q"], k_weight=weight["k"], interleaved=interleaved)
+    c.pa.check_pool()
+    pos = torch.arange(tokens, device="cuda")
+    check_rounded(q, *turned(x[:, :8], weight["q"], 1e-6, table, pos, interleaved))
+    want, slack = turned(x[:, 8:10], weight["k"], 1e-6, table, pos, interleaved)
+    if fp8:
+        kc, _, ks, _ = c.pa.gather_fp8(c.table[0], tokens)
+        check_fp8(kc, ks, want, slack)
+    else:
+        check_rounded(c.pa.gather(c.table[0], tokens)[0], want, slack)

@@ -27,7 +27,7 @@ def marked(c):
 def test_each_key_tile_has_its_part(heads, fp8, prior, nodes):
     """An element of the output is the weight of the tiles that mark it, and so is sum |w v|, so the bounds of tree_reference are relative ones: some 2^-8
     + 2^-7 (FP8 2^-8 + 2^-10) of an element.  A tile that is lost or taken twice changes its element by a twelfth at the least (64 dimensions,
-    eight tiles of 1 or 2); that the check sees one is shown on the reference."""
+    eight tiles of 1 or 2); that check_tree sees one is shown on the reference."""
     import torch
 
     c = Cache(*heads, np.add(prior, nodes), seed=41, fp8=fp8)
